@@ -21,9 +21,10 @@
  *
  * Around that layer the library also has, each documented at its declaration: the quantisation
  * step that produces the codes (Alg. 1 step 2.1), the layer's backward for multiplicative
- * fine-tuning of B and A (Sec. 3.4) and for quantisation-aware training (Eq. 4-5), and two
+ * fine-tuning of B and A (Sec. 3.4) and for quantisation-aware training (Eq. 4-5), two
  * comparators for the paper's efficiency table (a block-scaled layer, Eq. 2, and that layer with an
- * additive adapter).
+ * additive adapter), and linear layers in microscaled formats: 4-bit operands of the products of inference and
+ * training, 8-bit checkpoints of the activations for the gradients.
  *
  * Conventions
  *   - every function returns an int status: LORDS_OK (0) or a negative LORDS_ERR_*;
@@ -276,6 +277,88 @@ int lords_adapter_forward_f32(const void *x, const uint8_t *Qpacked, const void 
                               const float *codebook, int bits, int blk, int M, int m, int n, int r, float *y32, void *stream);
 
 /*
+ * Linear layers in microscaled formats (the OCP microscaling formats: 32 consecutive values of a row, a block, share a scale 2^E, held as
+ * E + 127 in a byte; 255 marks a block that is not a number).  Two formats:
+ *     4 bits: e2m1 values 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives (codes 0 .. 7; bit 3 is the sign); operands of products.
+ *             E = floor(log2 max|v|) - 2, so magnitudes between 6 and 8 times 2^E are limited to 6.
+ *     8 bits: whole numbers -127 .. 127, each standing for 1/64 of its value times 2^E; activations kept for the backward pass.
+ *             E = floor(log2 max|v|).
+ * In both E is at least -127, values round to the nearest, ties to the even code, and a block with an infinity or a NaN in it becomes not a number
+ * throughout (scale 255, codes 0).  Every value of either format is a bf16 number, so reading one back rounds nothing (but for
+ * magnitudes of 2^128 and more, which only scales above 252 that these calls do not write can make: they become infinite).
+ *
+ * Layout of a 4-bit tensor of rows x cols (lords_mxfp4_codes_bytes, lords_mxfp4_scales_bytes):
+ *   codes:  rows of ceil(cols / 32) * 16 bytes; column j in byte j / 2, the even column in the low nibble; zeros behind the last column.
+ *   scales: tiles of 128 rows x 4 blocks, 512 bytes each, the tiles of a row of tiles one after the other (the tensor cores take a tile in one
+ *           piece).  Row i, block b: byte ((i / 128) * ceil(blocks / 4) + b / 4) * 512 + (i % 32) * 16 + (i % 128) / 32 * 4 + b % 4.
+ *           The bytes behind the last row and block are 0.
+ *   (lords_mxfp4_quantize writes both whole.  Other writers have to write the zeros too: a 255 among them makes results not a number.)
+ * Layout of an 8-bit checkpoint of M x n (lords_checkpoint_bytes, lords_checkpoint_scales_bytes):
+ *   q: rows of ceil(n / 32) * 32 bytes (signed), zeros behind the last column;  e: rows of ceil(n / 128) * 4 bytes, a scale per block.
+ *
+ * All sizes are 1 to LORDS_MX_DIM_MAX, odd ones included; all pointers are on the device and 16-byte aligned (also where bytes are passed); matrices in bf16
+ * are dense.  The calls need lords_init on the calling thread's current device (LORDS_ERR_NOT_INIT otherwise), enqueue on `stream` and return without
+ * synchronising; unlike the weights of the layers above, everything here is read and written in the stream's order.
+ */
+#define LORDS_MX_DIM_MAX (1 << 20)
+
+/* Bytes of the two parts of a 4-bit tensor of rows x cols, or LORDS_ERR_SHAPE. */
+int64_t lords_mxfp4_codes_bytes(int64_t rows, int64_t cols);
+int64_t lords_mxfp4_scales_bytes(int64_t rows, int64_t cols);
+
+/*
+ * A tensor to 4 bits, along its rows, its columns, or both in one pass.
+ *   v                 : bf16 [rows][cols]
+ *   codes, scales     : the 4-bit tensor of rows x cols (blocks along a row), or both NULL
+ *   codes_t, scales_t : the 4-bit tensor of the transpose, cols x rows (blocks along a column of v), or both NULL
+ * What a product over the columns takes, and what one over the rows takes: with weights, activations and gradients brought to 4
+ * bits either way, lords_mxfp4_matmul gives a training step's three products (y = x W^T, dx = dy W, dW = dy^T x).
+ */
+int lords_mxfp4_quantize(const void *v, int rows, int cols, uint8_t *codes, uint8_t *scales, uint8_t *codes_t, uint8_t *scales_t,
+                         void *stream);
+
+/* The values of a 4-bit tensor: v, bf16 [rows][cols]. */
+int lords_mxfp4_dequantize(const uint8_t *codes, const uint8_t *scales, int rows, int cols, void *v, void *stream);
+
+/*
+ * y = x W^T on 4-bit operands, x: M x n and W: m x n, sums in fp32.
+ *   y : bf16 [M][m], rounded to nearest even, or float [M][m] for the _f32 variant
+ * Any product of two 4-bit tensors over their common axis; a block of either operand that is not a number makes the sums that it enters so.
+ */
+int lords_mxfp4_matmul(const uint8_t *x_codes, const uint8_t *x_scales, const uint8_t *w_codes, const uint8_t *w_scales, int M, int m,
+                       int n, void *y, void *stream);
+int lords_mxfp4_matmul_f32(const uint8_t *x_codes, const uint8_t *x_scales, const uint8_t *w_codes, const uint8_t *w_scales, int M, int m,
+                           int n, float *y32, void *stream);
+
+/*
+ * A layer held in 4 bits: x (bf16 [M][n]) is brought to 4 bits as lords_mxfp4_quantize does it, then y = x W^T as above.  The
+ * same results as those two calls, to the last bit.  Up to 16 tokens it is one launch without scratch memory; above, x in 4 bits lies in the
+ * lords_init workspace (as for the forward calls, two such calls may then only overlap if they are ordered on one stream).
+ */
+int lords_mxfp4_forward(const void *x, const uint8_t *w_codes, const uint8_t *w_scales, int M, int m, int n, void *y, void *stream);
+int lords_mxfp4_forward_f32(const void *x, const uint8_t *w_codes, const uint8_t *w_scales, int M, int m, int n, float *y32, void *stream);
+
+/* Bytes of the two parts of an 8-bit checkpoint of M x n, or LORDS_ERR_SHAPE. */
+int64_t lords_checkpoint_bytes(int64_t M, int64_t n);
+int64_t lords_checkpoint_scales_bytes(int64_t M, int64_t n);
+
+/* Activations x (bf16 [M][n]) to an 8-bit checkpoint (33/64 of the bytes), and the values of one back to bf16 [M][n]. */
+int lords_checkpoint_store(const void *x, int M, int n, uint8_t *q, uint8_t *e, void *stream);
+int lords_checkpoint_load(const uint8_t *q, const uint8_t *e, int M, int n, void *x, void *stream);
+
+/*
+ * lords_linear_backward_factors and lords_linear_backward_qat with the layer's input in an 8-bit checkpoint: the same gradients, to the last
+ * bit, as with the values of lords_checkpoint_load as x.  Those values lie in the lords_init workspace meanwhile (M * n * 2 bytes at its end,
+ * next to what the gradients take there; LORDS_ERR_WORKSPACE when there is no room for them).
+ */
+int lords_linear_backward_factors_checkpoint(const void *dy, const uint8_t *q, const uint8_t *e, const uint8_t *Qpacked, const void *B,
+                                             const void *A, const float *codebook, int bits, int M, int m, int n, int r, float *dB,
+                                             float *dA, void *stream);
+int lords_linear_backward_qat_checkpoint(const void *dy, const uint8_t *q, const uint8_t *e, const void *W, const uint8_t *Qpacked,
+                                         const void *B, const void *A, const float *codebook, int bits, int M, int m, int n, int r,
+                                         float *dW, float *dB, float *dA, void *stream);
+
+/*
  * Allocation-free forward (the paper has no counterpart: this is a deployment convenience).
  * For callers that must not allocate device memory -- for instance a plugin inside a server
  * whose memory pool already owns all of HBM, or a latency-critical loop that cannot take the
@@ -334,7 +417,7 @@ int lords_last_cuda_error(void);
 int lords_set_option(const char *key, const char *value);
 
 /* Name of the path the most recent call dispatched to ("simt", "decode", "decode16", "umma", "wide", "direct", "dense";
- * "quantize", "quantize_simt" for lords_quantize_codes).  A small layer that the direct kernel takes in place of the decode,
+ * "quantize", "quantize_simt" for lords_quantize_codes; "mxfp4_...", "checkpoint_..." for the microscaled formats).  A small layer that the direct kernel takes in place of the decode,
  * 16-token or scale-MMA kernel reports the name of the path it stands in for. */
 const char *lords_last_path(void);
 

@@ -41,6 +41,10 @@ def _load():
         "lords_strerror": (cs, [ci]),
         "lords_equivalent_rank": (i64, [i64, i64, i64]),
         "lords_packed_bytes": (i64, [i64, i64, ci]),
+        "lords_mxfp4_codes_bytes": (i64, [i64, i64]),
+        "lords_mxfp4_scales_bytes": (i64, [i64, i64]),
+        "lords_checkpoint_bytes": (i64, [i64, i64]),
+        "lords_checkpoint_scales_bytes": (i64, [i64, i64]),
         "lords_pack_codes": (ci, [p, i64, i64, ci, p]),
         "lords_unpack_codes": (ci, [p, i64, i64, ci, p]),
         "lords_init": (ci, [ci, sz]),
@@ -71,7 +75,10 @@ def exported_symbols():
             "lords_linear_forward", "lords_linear_forward_bits", "lords_linear_forward_f32",
             "lords_linear_forward_host", "lords_linear_forward_noalloc", "lords_quantize_codes", "lords_transpose_codes",
             "lords_linear_backward_input", "lords_linear_backward_input_f32", "lords_linear_backward_factors",
-            "lords_linear_backward_qat", "lords_blockscale_forward", "lords_blockscale_forward_f32", "lords_adapter_forward", "lords_adapter_forward_f32", "lords_poll_status", "lords_read_status_detail", "lords_last_cuda_error", "lords_set_option", "lords_last_path",
+            "lords_linear_backward_qat", "lords_mxfp4_codes_bytes", "lords_mxfp4_scales_bytes", "lords_mxfp4_quantize", "lords_mxfp4_dequantize",
+            "lords_mxfp4_matmul", "lords_mxfp4_matmul_f32", "lords_mxfp4_forward", "lords_mxfp4_forward_f32", "lords_checkpoint_bytes",
+            "lords_checkpoint_scales_bytes", "lords_checkpoint_store", "lords_checkpoint_load", "lords_linear_backward_factors_checkpoint",
+            "lords_linear_backward_qat_checkpoint", "lords_blockscale_forward", "lords_blockscale_forward_f32", "lords_adapter_forward", "lords_adapter_forward_f32", "lords_poll_status", "lords_read_status_detail", "lords_last_cuda_error", "lords_set_option", "lords_last_path",
             "lords_last_launch_count"]
 
 
@@ -100,6 +107,29 @@ def lords_packed_bytes(m: int, n: int, bits: int) -> int:
     if v < 0:
         raise LordsError(v, "lords_packed_bytes")
     return v
+
+
+def _bytes_of(name: str, rows: int, cols: int) -> int:
+    v = int(getattr(_load(), name)(rows, cols))
+    if v < 0:
+        raise LordsError(v, name)
+    return v
+
+
+def lords_mxfp4_codes_bytes(rows: int, cols: int) -> int:
+    return _bytes_of("lords_mxfp4_codes_bytes", rows, cols)
+
+
+def lords_mxfp4_scales_bytes(rows: int, cols: int) -> int:
+    return _bytes_of("lords_mxfp4_scales_bytes", rows, cols)
+
+
+def lords_checkpoint_bytes(M: int, n: int) -> int:
+    return _bytes_of("lords_checkpoint_bytes", M, n)
+
+
+def lords_checkpoint_scales_bytes(M: int, n: int) -> int:
+    return _bytes_of("lords_checkpoint_scales_bytes", M, n)
 
 
 def lords_pack_codes(codes: np.ndarray, bits: int) -> np.ndarray:
@@ -148,7 +178,9 @@ def _cb_ptr(codebook, bits):
 _TENSOR_CALLS = ("lords_linear_forward", "lords_linear_forward_bits", "lords_linear_forward_f32", "lords_linear_forward_host",
                  "lords_linear_forward_noalloc", "lords_quantize_codes", "lords_transpose_codes", "lords_linear_backward_input",
                  "lords_linear_backward_input_f32", "lords_linear_backward_factors", "lords_linear_backward_qat",
-                 "lords_blockscale_forward", "lords_adapter_forward")
+                 "lords_blockscale_forward", "lords_adapter_forward", "lords_mxfp4_quantize", "lords_mxfp4_dequantize", "lords_mxfp4_matmul",
+                 "lords_mxfp4_forward", "lords_checkpoint_store", "lords_checkpoint_load", "lords_linear_backward_factors_checkpoint",
+                 "lords_linear_backward_qat_checkpoint")
 
 
 def _native():

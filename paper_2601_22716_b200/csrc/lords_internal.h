@@ -131,6 +131,12 @@ int launch_backward_factors(const uint16_t *g, const uint16_t *x, const uint8_t 
                             const float *levels, int bits, int M, int m, int n, int r, float *dB, float *dA,
                             State &st, cudaStream_t stream);
 
+// What the entry points of both gradients ask of their arguments.
+int check_backward_factors(const void *dy, const void *x, const uint8_t *q, const void *B, const void *A, const float *codebook, int bits, int M, int m,
+                           int n, int r, const float *dB, const float *dA);
+int check_backward_qat(const void *dy, const void *x, const void *W, const uint8_t *q, const void *B, const void *A, const float *codebook, int bits, int M,
+                       int m, int n, int r, const float *dW, const float *dB, const float *dA);
+
 // Straight-through gradients of quantisation-aware training (Eq. 4-5): the tensor-core schedule where its
 // rules hold, else one pass over W per requested factor gradient on the CUDA cores.
 int launch_backward_qat(const uint16_t *g, const uint16_t *x, const uint16_t *W, const uint8_t *q, const uint16_t *B,
@@ -142,5 +148,23 @@ int launch_backward_qat(const uint16_t *g, const uint16_t *x, const uint16_t *W,
 int launch_blockscale16(const Problem &p, const uint16_t *scales, int blk, State &st, cudaStream_t stream);
 int launch_adapter(const uint16_t *x, const uint16_t *Al, const uint16_t *Bl, const float *y32, float *u, void *y, int y_f32,
                    int M, int m, int n, int r, cudaStream_t stream);
+
+// Microscaled formats (lords_mx.cuh).  One product y = x W^T on 4-bit operands, validated.
+struct MxProblem {
+    const uint16_t *x;       // bf16 [M][n], or null: x is in 4 bits already
+    const uint8_t *xq, *xs;  // codes and scale tiles of x
+    const uint8_t *w, *ws;   // codes and scale tiles of W
+    int M, m, n;
+    void *y;                 // bf16 [M][m] or float [M][m]
+    int y_f32;
+};
+int launch_mxfp4_quantize(const uint16_t *v, int rows, int cols, uint8_t *codes, uint8_t *scales, uint8_t *codes_t, uint8_t *scales_t, cudaStream_t stream);
+int launch_mxfp4_dequantize(const uint8_t *codes, const uint8_t *scales, int rows, int cols, uint16_t *v, cudaStream_t stream);
+// Few tokens: a CTA per 128 rows of W, the steps divided among a cluster.  x in bf16 (up to 16 tokens; else LORDS_ERR_UNSUPPORTED) or in 4 bits.
+int launch_mxfp4_stream(const MxProblem &p, State &st, cudaStream_t stream);
+
+// 8-bit checkpoints: rows of whole blocks, and scales four bytes per 128 columns.
+int launch_checkpoint_store(const uint16_t *x, int M, int n, uint8_t *q, uint8_t *e, cudaStream_t stream);
+int launch_checkpoint_load(const uint8_t *q, const uint8_t *e, int M, int n, uint16_t *x, int pitch, cudaStream_t stream);
 
 }  // namespace lords

@@ -335,6 +335,123 @@ PyObject *py_lords_adapter_forward(PyObject *, PyObject *const *args, Py_ssize_t
     return done(status, "lords_adapter_forward");
 }
 
+PyObject *py_lords_mxfp4_quantize(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyObject *kwnames)
+{
+    LORDS_ARGS("lords_mxfp4_quantize", 8, 5, "v", "rows", "cols", "codes", "scales", "codes_t", "scales_t", "stream");
+    int d[2];
+    void *v, *out[4], *s;
+    if (!to_int(a[1], &d[0]) || !to_int(a[2], &d[1]) || !to_ptr(a[0], false, &v) || !to_stream(a[7], &s)) return nullptr;
+    for (int k = 0; k < 4; ++k)
+        if (!to_ptr(a[3 + k], true, &out[k])) return nullptr;
+    LORDS_CALL(lords_mxfp4_quantize(v, d[0], d[1], static_cast<uint8_t *>(out[0]), static_cast<uint8_t *>(out[1]), static_cast<uint8_t *>(out[2]),
+                                    static_cast<uint8_t *>(out[3]), s));
+    return done(status, "lords_mxfp4_quantize");
+}
+
+typedef int (*FromFormatFn)(const uint8_t *, const uint8_t *, int, int, void *, void *);
+
+PyObject *from_format(const char *fn, FromFormatFn call, PyObject **a)
+{
+    int d[2];
+    void *q, *e, *v, *s;
+    if (!to_int(a[2], &d[0]) || !to_int(a[3], &d[1]) || !to_ptr(a[0], false, &q) || !to_ptr(a[1], false, &e) || !to_ptr(a[4], false, &v) || !to_stream(a[5], &s))
+        return nullptr;
+    LORDS_CALL(call(static_cast<const uint8_t *>(q), static_cast<const uint8_t *>(e), d[0], d[1], v, s));
+    return done(status, fn);
+}
+
+PyObject *py_lords_mxfp4_dequantize(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyObject *kwnames)
+{
+    LORDS_ARGS("lords_mxfp4_dequantize", 6, 5, "codes", "scales", "rows", "cols", "v", "stream");
+    return from_format("lords_mxfp4_dequantize", lords_mxfp4_dequantize, a);
+}
+
+PyObject *py_lords_checkpoint_load(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyObject *kwnames)
+{
+    LORDS_ARGS("lords_checkpoint_load", 6, 5, "q", "e", "M", "n", "x", "stream");
+    return from_format("lords_checkpoint_load", lords_checkpoint_load, a);
+}
+
+PyObject *py_lords_checkpoint_store(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyObject *kwnames)
+{
+    LORDS_ARGS("lords_checkpoint_store", 6, 5, "x", "M", "n", "q", "e", "stream");
+    int d[2];
+    void *x, *q, *e, *s;
+    if (!to_int(a[1], &d[0]) || !to_int(a[2], &d[1]) || !to_ptr(a[0], false, &x) || !to_ptr(a[3], false, &q) || !to_ptr(a[4], false, &e) || !to_stream(a[5], &s))
+        return nullptr;
+    LORDS_CALL(lords_checkpoint_store(x, d[0], d[1], static_cast<uint8_t *>(q), static_cast<uint8_t *>(e), s));
+    return done(status, "lords_checkpoint_store");
+}
+
+PyObject *py_lords_mxfp4_matmul(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyObject *kwnames)
+{
+    LORDS_ARGS("lords_mxfp4_matmul", 10, 8, "x_codes", "x_scales", "w_codes", "w_scales", "M", "m", "n", "y", "stream", "f32");
+    int d[3];
+    void *p[4], *y, *s;
+    for (int k = 0; k < 3; ++k)
+        if (!to_int(a[4 + k], &d[k])) return nullptr;
+    for (int k = 0; k < 4; ++k)
+        if (!to_ptr(a[k], false, &p[k])) return nullptr;
+    const int f32 = a[9] ? PyObject_IsTrue(a[9]) : 0;
+    if (f32 < 0 || !to_ptr(a[7], false, &y) || !to_stream(a[8], &s)) return nullptr;
+    const uint8_t *xq = static_cast<const uint8_t *>(p[0]), *xs = static_cast<const uint8_t *>(p[1]), *w = static_cast<const uint8_t *>(p[2]),
+                  *ws = static_cast<const uint8_t *>(p[3]);
+    LORDS_CALL(f32 ? lords_mxfp4_matmul_f32(xq, xs, w, ws, d[0], d[1], d[2], static_cast<float *>(y), s) : lords_mxfp4_matmul(xq, xs, w, ws, d[0], d[1], d[2], y, s));
+    return done(status, "lords_mxfp4_matmul");
+}
+
+PyObject *py_lords_mxfp4_forward(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyObject *kwnames)
+{
+    LORDS_ARGS("lords_mxfp4_forward", 9, 7, "x", "w_codes", "w_scales", "M", "m", "n", "y", "stream", "f32");
+    int d[3];
+    void *p[3], *y, *s;
+    for (int k = 0; k < 3; ++k)
+        if (!to_int(a[3 + k], &d[k]) || !to_ptr(a[k], false, &p[k])) return nullptr;
+    const int f32 = a[8] ? PyObject_IsTrue(a[8]) : 0;
+    if (f32 < 0 || !to_ptr(a[6], false, &y) || !to_stream(a[7], &s)) return nullptr;
+    const uint8_t *w = static_cast<const uint8_t *>(p[1]), *ws = static_cast<const uint8_t *>(p[2]);
+    LORDS_CALL(f32 ? lords_mxfp4_forward_f32(p[0], w, ws, d[0], d[1], d[2], static_cast<float *>(y), s) : lords_mxfp4_forward(p[0], w, ws, d[0], d[1], d[2], y, s));
+    return done(status, "lords_mxfp4_forward");
+}
+
+PyObject *py_lords_linear_backward_factors_checkpoint(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyObject *kwnames)
+{
+    LORDS_ARGS("lords_linear_backward_factors_checkpoint", 15, 14, "dy", "q", "e", "Qpacked", "B", "A", "codebook", "bits", "M", "m", "n", "r", "dB", "dA",
+               "stream");
+    int v[5];
+    void *p[6], *dB, *dA, *s;
+    Table cb;
+    for (int k = 0; k < 5; ++k)
+        if (!to_int(a[7 + k], &v[k])) return nullptr;
+    for (int k = 0; k < 6; ++k)
+        if (!to_ptr(a[k], false, &p[k])) return nullptr;
+    if (!cb.read(a[6], v[0]) || !to_ptr(a[12], true, &dB) || !to_ptr(a[13], true, &dA) || !to_stream(a[14], &s)) return nullptr;
+    LORDS_CALL(lords_linear_backward_factors_checkpoint(p[0], static_cast<const uint8_t *>(p[1]), static_cast<const uint8_t *>(p[2]),
+                                                        static_cast<const uint8_t *>(p[3]), p[4], p[5], cb.data(), v[0], v[1], v[2], v[3], v[4],
+                                                        static_cast<float *>(dB), static_cast<float *>(dA), s));
+    return done(status, "lords_linear_backward_factors_checkpoint");
+}
+
+PyObject *py_lords_linear_backward_qat_checkpoint(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyObject *kwnames)
+{
+    LORDS_ARGS("lords_linear_backward_qat_checkpoint", 17, 16, "dy", "q", "e", "W", "Qpacked", "B", "A", "codebook", "bits", "M", "m", "n", "r", "dW", "dB",
+               "dA", "stream");
+    int v[5];
+    void *p[7], *out[3], *s;
+    Table cb;
+    for (int k = 0; k < 5; ++k)
+        if (!to_int(a[8 + k], &v[k])) return nullptr;
+    for (int k = 0; k < 7; ++k)
+        if (!to_ptr(a[k], false, &p[k])) return nullptr;
+    for (int k = 0; k < 3; ++k)
+        if (!to_ptr(a[13 + k], true, &out[k])) return nullptr;
+    if (!cb.read(a[7], v[0]) || !to_stream(a[16], &s)) return nullptr;
+    LORDS_CALL(lords_linear_backward_qat_checkpoint(p[0], static_cast<const uint8_t *>(p[1]), static_cast<const uint8_t *>(p[2]), p[3],
+                                                    static_cast<const uint8_t *>(p[4]), p[5], p[6], cb.data(), v[0], v[1], v[2], v[3], v[4],
+                                                    static_cast<float *>(out[0]), static_cast<float *>(out[1]), static_cast<float *>(out[2]), s));
+    return done(status, "lords_linear_backward_qat_checkpoint");
+}
+
 PyObject *py_setup(PyObject *, PyObject *args)
 {
     PyObject *error, *table;
@@ -376,6 +493,24 @@ PyMethodDef g_methods[] = {
               "Comparator (Eq. 2): y = x (L[Q] (.) (s (x) 1))^T; y is bf16 [M, m], or float with f32=True."),
     LORDS_DEF(lords_adapter_forward, "lords_adapter_forward(x, Qpacked, scales, A_l, B_l, codebook, bits, blk, M, m, n, r, y, stream=None, f32=False)\n--\n\n"
               "Comparator (Sec. 3.4 / 4.4): the block-scaled layer plus an additive rank-r adapter, three launches."),
+    LORDS_DEF(lords_mxfp4_quantize, "lords_mxfp4_quantize(v, rows, cols, codes, scales, codes_t=None, scales_t=None, stream=None)\n--\n\n"
+              "bf16 [rows, cols] to 4 bits in blocks along the rows (codes, scales) and / or along the columns (codes_t, scales_t); either pair may be None."),
+    LORDS_DEF(lords_mxfp4_dequantize, "lords_mxfp4_dequantize(codes, scales, rows, cols, v, stream=None)\n--\n\n"
+              "The values of a 4-bit tensor, bf16 [rows, cols]."),
+    LORDS_DEF(lords_mxfp4_matmul, "lords_mxfp4_matmul(x_codes, x_scales, w_codes, w_scales, M, m, n, y, stream=None, f32=False)\n--\n\n"
+              "y = x W^T on 4-bit operands (x: M x n, W: m x n); y is bf16 [M, m], or float with f32=True."),
+    LORDS_DEF(lords_mxfp4_forward, "lords_mxfp4_forward(x, w_codes, w_scales, M, m, n, y, stream=None, f32=False)\n--\n\n"
+              "The layer with bf16 activations x[M,n], which the call brings to 4 bits."),
+    LORDS_DEF(lords_checkpoint_store, "lords_checkpoint_store(x, M, n, q, e, stream=None)\n--\n\n"
+              "Activations bf16 [M, n] to an 8-bit checkpoint (values q, scales e)."),
+    LORDS_DEF(lords_checkpoint_load, "lords_checkpoint_load(q, e, M, n, x, stream=None)\n--\n\n"
+              "The values of an 8-bit checkpoint, bf16 [M, n]."),
+    LORDS_DEF(lords_linear_backward_factors_checkpoint,
+              "lords_linear_backward_factors_checkpoint(dy, q, e, Qpacked, B, A, codebook, bits, M, m, n, r, dB, dA, stream=None)\n--\n\n"
+              "lords_linear_backward_factors with the layer's input in an 8-bit checkpoint."),
+    LORDS_DEF(lords_linear_backward_qat_checkpoint,
+              "lords_linear_backward_qat_checkpoint(dy, q, e, W, Qpacked, B, A, codebook, bits, M, m, n, r, dW, dB, dA, stream=None)\n--\n\n"
+              "lords_linear_backward_qat with the layer's input in an 8-bit checkpoint."),
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_native", "Native calls of the LoRDS library (see binding.py).", -1, g_methods,

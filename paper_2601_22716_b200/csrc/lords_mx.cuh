@@ -1,0 +1,125 @@
+// Device-side helpers of the microscaled formats: blocks of 32 values that share a scale 2^E (the OCP microscaling formats).
+//
+//   4 bits: e2m1 values (0, 0.5, 1, 1.5, 2, 3, 4, 6, sign in bit 3), E = floor(log2 of the largest magnitude) - 2
+//   8 bits: whole numbers -127 .. 127 in steps of 1/64,               E = floor(log2 of the largest magnitude)
+//
+// E is at least -127 and is held as E + 127 in a byte; 255 stands for "not a number" and marks a block in which a value is not finite.  Values
+// are bf16, whose exponent field gives E at once, and a division by 2^E is exact, so the only rounding is the one to the
+// format's values: to nearest, ties to the even code, the magnitude limited to 6 and 127/64.
+#pragma once
+
+#include <stdint.h>
+
+#include "lords_ptx.cuh"
+
+namespace lords {
+namespace mx {
+
+constexpr int kBlock = 32;                  // values that share a scale
+constexpr int kTileRows = 128;              // rows of a tile of 4-bit scales ...
+constexpr int kTileBlocks = 4;              // ... and blocks: what one copy into TMEM takes
+constexpr int kTileBytes = kTileRows * kTileBlocks;
+
+__host__ __device__ inline int blocks_of(int cols) { return (cols + kBlock - 1) / kBlock; }
+__host__ __device__ inline int scale_tiles_of(int cols) { return (blocks_of(cols) + kTileBlocks - 1) / kTileBlocks; }
+__host__ __device__ inline size_t codes_pitch(int cols) { return (size_t)blocks_of(cols) * 16; }
+
+// Where the scale of row i and block b of a tile lies inside it: four words a lane, a word the four blocks of row 32 j + lane.
+__host__ __device__ inline int scale_at(int i, int b) { return (i & 31) * 16 + (i >> 5) * 4 + b; }
+
+// The larger of two pairs of bf16 magnitudes.  As whole numbers they are in order, infinities and NaNs above all others.
+__device__ __forceinline__ uint32_t max_magnitudes(uint32_t top, uint32_t pair) { return __vmaxu2(top, pair & 0x7FFF7FFFu); }
+
+// Scale byte from the bf16 pattern of the block's largest magnitude; BELOW: 2 for the 4-bit, 0 for the 8-bit format.
+template <int BELOW> __device__ __forceinline__ uint32_t scale_byte(uint32_t top)
+{
+    const uint32_t ex = top >> 7;
+    return ex == 255u ? 255u : ex > (uint32_t)BELOW ? ex - (uint32_t)BELOW : 0u;
+}
+// 2^-E (zero for a block that is not finite: every code is 0 there)
+__device__ __forceinline__ float inverse_scale(uint32_t byte)
+{
+    return byte == 255u ? 0.0f : byte == 254u ? __uint_as_float(0x00400000u) : __uint_as_float((254u - byte) << 23);
+}
+
+// Eight bf16 values (pairs, low half first), times 2^-E, to eight 4-bit codes, low nibble first.
+__device__ __forceinline__ uint32_t to_codes4(const uint32_t (&w)[4], float inv)
+{
+    float v[8];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        v[2 * k] = __uint_as_float(w[k] << 16) * inv;
+        v[2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u) * inv;
+    }
+    uint32_t c;
+    asm("{\n"
+        ".reg .b8 b0, b1, b2, b3;\n"
+        "cvt.rn.satfinite.e2m1x2.f32 b0, %2, %1;\n"
+        "cvt.rn.satfinite.e2m1x2.f32 b1, %4, %3;\n"
+        "cvt.rn.satfinite.e2m1x2.f32 b2, %6, %5;\n"
+        "cvt.rn.satfinite.e2m1x2.f32 b3, %8, %7;\n"
+        "mov.b32 %0, {b0, b1, b2, b3};\n"
+        "}\n"
+        : "=r"(c)
+        : "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]));
+    return c;
+}
+// (infinity and NaN times the zero that stands for 2^-E of such a block are NaN, which the conversion makes 6)
+__device__ __forceinline__ uint32_t to_codes4(const uint32_t (&w)[4], uint32_t byte)
+{
+    const uint32_t c = to_codes4(w, inverse_scale(byte));
+    return byte == 255u ? 0u : c;
+}
+
+}  // namespace mx
+
+namespace ptx {
+
+// A copy of whole 16-byte words from global into this CTA's shared memory, its bytes counted on `bar`.
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar)
+                 : "memory");
+}
+// A tile of scales (512 bytes, 32 rows of 16) into four TMEM columns, the 32 lanes repeated in all four quadrants; ordered before the MMAs that
+// the same thread issues next, and after those it has issued.
+__device__ __forceinline__ void scales_to_tmem(uint32_t taddr, uint64_t desc, uint32_t leader)
+{
+    asm volatile(
+        "{\n"
+        ".reg .pred q;\n"
+        "setp.ne.b32 q, %2, 0;\n"
+        "@q tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;\n"
+        "}\n" ::"r"(taddr), "l"(desc), "r"(leader)
+        : "memory");
+}
+// Descriptor of such a tile: no swizzle, groups of 8 rows 128 bytes apart.
+__device__ __forceinline__ uint64_t scales_desc(uint32_t smem_addr)
+{
+    return (uint64_t)((smem_addr & 0x3FFFFu) >> 4) | ((uint64_t)1 << 16) | ((uint64_t)8 << 32) | ((uint64_t)1 << 46);
+}
+// Instruction descriptor of kind::mxf4: e2m1 operands, both K-major, scales 2^E, 64 values of K, two blocks of each row.  The scales' place in their
+// TMEM words (the low or the high two bytes) is `half` = 0 or 1.
+__host__ __device__ constexpr uint32_t umma_idesc_mxf4(int M, int N, int half)
+{
+    return ((uint32_t)(2 * half) << 4)        // B's scales: byte 0 or 2
+           | (1u << 7) | (1u << 10)           // e2m1
+           | ((uint32_t)(N >> 3) << 17) | (1u << 23)      // scales are powers of two
+           | ((uint32_t)(M >> 4) << 24) | ((uint32_t)(2 * half) << 29);
+}
+// D[tmem] (+)= (A[smem] with its scales) * (B[smem] with its scales)
+__device__ __forceinline__ void umma_mxf4_ss(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t sa_tmem, uint32_t sb_tmem,
+                                             uint32_t accumulate, uint32_t leader)
+{
+    asm volatile(
+        "{\n"
+        ".reg .pred p, q;\n"
+        "setp.ne.b32 p, %6, 0;\n"
+        "setp.ne.b32 q, %7, 0;\n"
+        "@q tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n"
+        "}\n" ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(sa_tmem), "r"(sb_tmem), "r"(accumulate), "r"(leader)
+        : "memory");
+}
+
+}  // namespace ptx
+}  // namespace lords

@@ -1,0 +1,159 @@
+// Tensors to and from the microscaled formats of lords_mx.cuh.
+//
+// Each kernel reads its input once and is bound by the bytes it moves.
+#include <cuda_bf16.h>
+
+#include "lords_internal.h"
+#include "lords_mx.cuh"
+#include "lords_tc_common.cuh"
+
+namespace lords {
+
+namespace {
+
+using namespace mx;
+
+// ------------------------------------------------------------------------------------------------ to 4 bits
+// A CTA takes 128 rows x 128 columns: one whole tile of scales in either orientation.  Along the rows, four neighbouring threads hold a block in
+// registers.  Along the columns, a thread reads two columns x 32 rows back from shared memory.
+constexpr int kQThreads = 256;
+constexpr int kQPitch = 128 * 2 + 16;       // bytes per row of the tile in shared memory; 16-byte words stay aligned
+
+// Eight values of row i from column c on as pairs, zeros outside the matrix.
+__device__ __forceinline__ void load8(const uint16_t *__restrict__ v, int rows, int cols, int i, int c, uint32_t (&w)[4])
+{
+#pragma unroll
+    for (int k = 0; k < 4; ++k) w[k] = 0u;
+    if (i >= rows || c >= cols) return;
+    const uint16_t *src = v + (size_t)i * cols + c;
+    if ((cols & 7) == 0) {
+        const uint4 q = __ldg(reinterpret_cast<const uint4 *>(src));
+        w[0] = q.x; w[1] = q.y; w[2] = q.z; w[3] = q.w;
+    } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const uint32_t lo = c + 2 * k < cols ? __ldg(src + 2 * k) : 0u, hi = c + 2 * k + 1 < cols ? __ldg(src + 2 * k + 1) : 0u;
+            w[k] = lo | hi << 16;
+        }
+    }
+}
+
+struct QuantizeParams {
+    const uint16_t *v;       // bf16 [rows][cols]
+    uint8_t *codes, *scales;         // blocks along the rows (null: not asked for)
+    uint8_t *codes_t, *scales_t;     // blocks along the columns: the same for the transposed matrix (null: not asked for)
+    int rows, cols;
+};
+
+__global__ void __launch_bounds__(kQThreads) lords_mxfp4_quantize_kernel(const QuantizeParams p)
+{
+    __shared__ __align__(16) uint8_t tile[128 * kQPitch];
+    __shared__ __align__(16) uint8_t sc[kTileBytes], sct[kTileBytes];
+    const int tid = threadIdx.x, r0 = (int)blockIdx.y * 128, c0 = (int)blockIdx.x * 128;
+    const int seg = tid & 15, row_in = tid >> 4;
+    uint32_t w[8][4];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) load8(p.v, p.rows, p.cols, r0 + k * 16 + row_in, c0 + seg * 8, w[k]);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        const int rl = k * 16 + row_in;
+        if (p.codes_t) *reinterpret_cast<uint4 *>(tile + rl * kQPitch + seg * 16) = make_uint4(w[k][0], w[k][1], w[k][2], w[k][3]);
+        if (p.codes) {
+            uint32_t top = max_magnitudes(max_magnitudes(max_magnitudes(max_magnitudes(0u, w[k][0]), w[k][1]), w[k][2]), w[k][3]);
+            top = __vmaxu2(top, __shfl_xor_sync(0xffffffffu, top, 1));
+            top = __vmaxu2(top, __shfl_xor_sync(0xffffffffu, top, 2));
+            const uint32_t byte = scale_byte<2>(max(top & 0xFFFFu, top >> 16));
+            const int c = c0 + seg * 8;
+            if (r0 + rl < p.rows && c < (int)codes_pitch(p.cols) * 2)
+                *reinterpret_cast<uint32_t *>(p.codes + (size_t)(r0 + rl) * codes_pitch(p.cols) + c / 2) = to_codes4(w[k], byte);
+            if ((seg & 3) == 0) sc[scale_at(rl, seg >> 2)] = (uint8_t)byte;
+        }
+    }
+    __syncthreads();
+    if (p.codes && tid < kTileBytes / 16)
+        reinterpret_cast<uint4 *>(p.scales + ((size_t)blockIdx.y * scale_tiles_of(p.cols) + blockIdx.x) * kTileBytes)[tid] = reinterpret_cast<const uint4 *>(sc)[tid];
+    if (!p.codes_t) return;
+    {
+        const int pair = tid & 63, b = tid >> 6;        // two columns, a block of 32 rows
+        uint32_t u[32];
+        uint32_t top = 0u;
+#pragma unroll
+        for (int k = 0; k < 32; ++k) {
+            u[k] = *reinterpret_cast<const uint32_t *>(tile + (b * 32 + k) * kQPitch + pair * 4);
+            top = max_magnitudes(top, u[k]);
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const uint32_t byte = scale_byte<2>(h ? top >> 16 : top & 0xFFFFu);
+            uint32_t out[4];
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                uint32_t x[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) x[k] = __byte_perm(u[8 * g + 2 * k], u[8 * g + 2 * k + 1], h ? 0x7632 : 0x5410);
+                out[g] = to_codes4(x, byte);
+            }
+            const int col = c0 + 2 * pair + h, r = r0 + b * 32;
+            if (col < p.cols && r < p.rows)
+                *reinterpret_cast<uint4 *>(p.codes_t + (size_t)col * codes_pitch(p.rows) + r / 2) = make_uint4(out[0], out[1], out[2], out[3]);
+            sct[scale_at(2 * pair + h, b)] = (uint8_t)byte;
+        }
+    }
+    __syncthreads();
+    if (tid < kTileBytes / 16)
+        reinterpret_cast<uint4 *>(p.scales_t + ((size_t)blockIdx.x * scale_tiles_of(p.rows) + blockIdx.y) * kTileBytes)[tid] = reinterpret_cast<const uint4 *>(sct)[tid];
+}
+
+// ----------------------------------------------------------------------------------------------- from 4 bits
+// Eight values a thread.  A value times 2^E is a bf16 number (two significant bits, at least 2^-128), so nothing is rounded.
+__global__ void __launch_bounds__(256) lords_mxfp4_dequantize_kernel(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scales, int rows, int cols,
+                                                                     uint16_t *__restrict__ v)
+{
+    const int c = ((int)blockIdx.x * 256 + (int)threadIdx.x) * 8, i = (int)blockIdx.y;
+    if (c >= cols) return;
+    for (int row = i; row < rows; row += gridDim.y) {
+        const uint32_t w = __ldg(reinterpret_cast<const uint32_t *>(codes + (size_t)row * codes_pitch(cols) + c / 2));
+        const int b = c / kBlock;
+        const uint32_t e = __ldg(scales + ((size_t)(row / kTileRows) * scale_tiles_of(cols) + b / kTileBlocks) * kTileBytes + scale_at(row % kTileRows, b % kTileBlocks));
+        // half the scale, so that 2^-127 stays a normal number: the values below are doubled (0, 1, 2, 3, 4, 6, 8, 12)
+        const float s = e == 255u ? __uint_as_float(0x7FC00000u) : e > 1u ? __uint_as_float((e - 1u) << 23) : e == 1u ? __uint_as_float(0x00400000u) : __uint_as_float(0x00200000u);
+        uint16_t out[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const uint32_t code = w >> (4 * k) & 15u, m = code & 7u;
+            const float d = (float)(m < 4u ? m : m == 4u ? 4u : m == 5u ? 6u : m == 6u ? 8u : 12u);
+            const float f = d * s;
+            out[k] = (uint16_t)((__float_as_uint(f) >> 16) | (code & 8u) << 12);
+        }
+        uint16_t *dst = v + (size_t)row * cols + c;
+        if ((cols & 7) == 0) {
+            *reinterpret_cast<uint4 *>(dst) = make_uint4(out[0] | (uint32_t)out[1] << 16, out[2] | (uint32_t)out[3] << 16, out[4] | (uint32_t)out[5] << 16, out[6] | (uint32_t)out[7] << 16);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (c + k < cols) dst[k] = out[k];
+        }
+    }
+}
+
+}  // namespace
+
+int launch_mxfp4_quantize(const uint16_t *v, int rows, int cols, uint8_t *codes, uint8_t *scales, uint8_t *codes_t, uint8_t *scales_t, cudaStream_t stream)
+{
+    const QuantizeParams p = {v, codes, scales, codes_t, scales_t, rows, cols};
+    const dim3 grid((unsigned)((cols + 127) / 128), (unsigned)((rows + 127) / 128));
+    if (grid.y > 65535u) return LORDS_ERR_SHAPE;
+    lords_mxfp4_quantize_kernel<<<grid, kQThreads, 0, stream>>>(p);
+    LORDS_CUDA_TRY(cudaGetLastError());
+    return LORDS_OK;
+}
+
+int launch_mxfp4_dequantize(const uint8_t *codes, const uint8_t *scales, int rows, int cols, uint16_t *v, cudaStream_t stream)
+{
+    const dim3 grid((unsigned)((cols + 2047) / 2048), (unsigned)(rows < 65535 ? rows : 65535));
+    lords_mxfp4_dequantize_kernel<<<grid, 256, 0, stream>>>(codes, scales, rows, cols, v);
+    LORDS_CUDA_TRY(cudaGetLastError());
+    return LORDS_OK;
+}
+
+}  // namespace lords
