@@ -162,6 +162,8 @@ int launch_mxfp4_quantize(const uint16_t *v, int rows, int cols, uint8_t *codes,
 int launch_mxfp4_dequantize(const uint8_t *codes, const uint8_t *scales, int rows, int cols, uint16_t *v, cudaStream_t stream);
 // Few tokens: a CTA per 128 rows of W, the steps divided among a cluster.  x in bf16 (up to 16 tokens; else LORDS_ERR_UNSUPPORTED) or in 4 bits.
 int launch_mxfp4_stream(const MxProblem &p, State &st, cudaStream_t stream);
+// Many tokens: CTA pairs, 256 tokens x 128 or 256 out-features.  x in 4 bits.
+int launch_mxfp4_pair(const MxProblem &p, State &st, cudaStream_t stream);
 
 // 8-bit checkpoints: rows of whole blocks, and scales four bytes per 128 columns.
 int launch_checkpoint_store(const uint16_t *x, int M, int n, uint8_t *q, uint8_t *e, cudaStream_t stream);

@@ -93,6 +93,17 @@ __device__ __forceinline__ void scales_to_tmem(uint32_t taddr, uint64_t desc, ui
         "}\n" ::"r"(taddr), "l"(desc), "r"(leader)
         : "memory");
 }
+// The same in both CTAs of a pair, each from its own shared memory at the same offset; one thread of the even CTA.
+__device__ __forceinline__ void scales_to_tmem2(uint32_t taddr, uint64_t desc, uint32_t leader)
+{
+    asm volatile(
+        "{\n"
+        ".reg .pred q;\n"
+        "setp.ne.b32 q, %2, 0;\n"
+        "@q tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;\n"
+        "}\n" ::"r"(taddr), "l"(desc), "r"(leader)
+        : "memory");
+}
 // Descriptor of such a tile: no swizzle, groups of 8 rows 128 bytes apart.
 __device__ __forceinline__ uint64_t scales_desc(uint32_t smem_addr)
 {
@@ -117,6 +128,19 @@ __device__ __forceinline__ void umma_mxf4_ss(uint32_t d_tmem, uint64_t a_desc, u
         "setp.ne.b32 p, %6, 0;\n"
         "setp.ne.b32 q, %7, 0;\n"
         "@q tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n"
+        "}\n" ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(sa_tmem), "r"(sb_tmem), "r"(accumulate), "r"(leader)
+        : "memory");
+}
+// The same on a CTA pair: each CTA holds half of A's rows with their scales, half of B's rows, and the scales of all of B's rows.
+__device__ __forceinline__ void umma2_mxf4_ss(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t sa_tmem, uint32_t sb_tmem,
+                                              uint32_t accumulate, uint32_t leader)
+{
+    asm volatile(
+        "{\n"
+        ".reg .pred p, q;\n"
+        "setp.ne.b32 p, %6, 0;\n"
+        "setp.ne.b32 q, %7, 0;\n"
+        "@q tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n"
         "}\n" ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(sa_tmem), "r"(sb_tmem), "r"(accumulate), "r"(leader)
         : "memory");
 }

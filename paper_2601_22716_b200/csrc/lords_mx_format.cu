@@ -45,9 +45,9 @@ struct QuantizeParams {
     int rows, cols;
 };
 
-__global__ void __launch_bounds__(kQThreads) lords_mxfp4_quantize_kernel(const QuantizeParams p)
+template <bool ALONG, bool ACROSS> __global__ void __launch_bounds__(kQThreads) lords_mxfp4_quantize_kernel(const QuantizeParams p)
 {
-    __shared__ __align__(16) uint8_t tile[128 * kQPitch];
+    __shared__ __align__(16) uint8_t tile[ACROSS ? 128 * kQPitch : 16];
     __shared__ __align__(16) uint8_t sc[kTileBytes], sct[kTileBytes];
     const int tid = threadIdx.x, r0 = (int)blockIdx.y * 128, c0 = (int)blockIdx.x * 128;
     const int seg = tid & 15, row_in = tid >> 4;
@@ -57,8 +57,8 @@ __global__ void __launch_bounds__(kQThreads) lords_mxfp4_quantize_kernel(const Q
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
         const int rl = k * 16 + row_in;
-        if (p.codes_t) *reinterpret_cast<uint4 *>(tile + rl * kQPitch + seg * 16) = make_uint4(w[k][0], w[k][1], w[k][2], w[k][3]);
-        if (p.codes) {
+        if constexpr (ACROSS) *reinterpret_cast<uint4 *>(tile + rl * kQPitch + seg * 16) = make_uint4(w[k][0], w[k][1], w[k][2], w[k][3]);
+        if constexpr (ALONG) {
             uint32_t top = max_magnitudes(max_magnitudes(max_magnitudes(max_magnitudes(0u, w[k][0]), w[k][1]), w[k][2]), w[k][3]);
             top = __vmaxu2(top, __shfl_xor_sync(0xffffffffu, top, 1));
             top = __vmaxu2(top, __shfl_xor_sync(0xffffffffu, top, 2));
@@ -70,9 +70,9 @@ __global__ void __launch_bounds__(kQThreads) lords_mxfp4_quantize_kernel(const Q
         }
     }
     __syncthreads();
-    if (p.codes && tid < kTileBytes / 16)
+    if (ALONG && tid < kTileBytes / 16)
         reinterpret_cast<uint4 *>(p.scales + ((size_t)blockIdx.y * scale_tiles_of(p.cols) + blockIdx.x) * kTileBytes)[tid] = reinterpret_cast<const uint4 *>(sc)[tid];
-    if (!p.codes_t) return;
+    if constexpr (!ACROSS) return;
     {
         const int pair = tid & 63, b = tid >> 6;        // two columns, a block of 32 rows
         uint32_t u[32];
@@ -105,33 +105,60 @@ __global__ void __launch_bounds__(kQThreads) lords_mxfp4_quantize_kernel(const Q
 }
 
 // ----------------------------------------------------------------------------------------------- from 4 bits
-// Eight values a thread.  A value times 2^E is a bf16 number (two significant bits, at least 2^-128), so nothing is rounded.
-__global__ void __launch_bounds__(256) lords_mxfp4_dequantize_kernel(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scales, int rows, int cols,
-                                                                     uint16_t *__restrict__ v)
+// A code's three low bits are a bf16 exponent's last two bits and the first of its mantissa, less 126 in the exponent: moved there and multiplied by 2^126,
+// and by 2^E then, both exactly (zero and a half too, as a subnormal number times 2^126).  Two codes at a time; the word's nibbles k and
+// k + 4 are taken together.
+__device__ __forceinline__ uint32_t bf16x2_mul(uint32_t a, uint32_t b)
 {
-    const int c = ((int)blockIdx.x * 256 + (int)threadIdx.x) * 8, i = (int)blockIdx.y;
+    uint32_t d;
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+__device__ __forceinline__ uint4 values4(uint32_t w, uint32_t byte)
+{
+    // 2^E as a bf16 number: 2^-127 is subnormal, and the pattern of a NaN stands for 255
+    const uint32_t s = byte == 255u ? 0x7FC0u : byte == 0u ? 0x0040u : byte << 7, ss = s | s << 16;
+    uint32_t v[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const uint32_t sign = k < 3 ? w << (12 - 4 * k) : w, mag = k < 2 ? w << (6 - 4 * k) : w >> (4 * k - 6);
+        v[k] = bf16x2_mul(bf16x2_mul((sign & 0x80008000u) | (mag & 0x01C001C0u), 0x7E807E80u), ss);
+    }
+    return make_uint4(__byte_perm(v[0], v[1], 0x5410), __byte_perm(v[2], v[3], 0x5410), __byte_perm(v[0], v[1], 0x7632), __byte_perm(v[2], v[3], 0x7632));
+}
+
+// A CTA takes 128 rows x 256 columns, a warp four rows at a time, a thread eight values of each.
+constexpr int kDThreads = 256, kDRows = 4;
+__global__ void __launch_bounds__(kDThreads) lords_mxfp4_dequantize_kernel(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scales, int rows,
+                                                                           int cols, uint16_t *__restrict__ v)
+{
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int c = (int)blockIdx.x * 256 + lane * 8, r0 = (int)blockIdx.y * kTileRows, b = c / kBlock;
     if (c >= cols) return;
-    for (int row = i; row < rows; row += gridDim.y) {
-        const uint32_t w = __ldg(reinterpret_cast<const uint32_t *>(codes + (size_t)row * codes_pitch(cols) + c / 2));
-        const int b = c / kBlock;
-        const uint32_t e = __ldg(scales + ((size_t)(row / kTileRows) * scale_tiles_of(cols) + b / kTileBlocks) * kTileBytes + scale_at(row % kTileRows, b % kTileBlocks));
-        // half the scale, so that 2^-127 stays a normal number: the values below are doubled (0, 1, 2, 3, 4, 6, 8, 12)
-        const float s = e == 255u ? __uint_as_float(0x7FC00000u) : e > 1u ? __uint_as_float((e - 1u) << 23) : e == 1u ? __uint_as_float(0x00400000u) : __uint_as_float(0x00200000u);
-        uint16_t out[8];
+    const size_t pitch = codes_pitch(cols);
+    const uint8_t *sc = scales + ((size_t)blockIdx.y * scale_tiles_of(cols) + b / kTileBlocks) * kTileBytes;
+#pragma unroll 1
+    for (int r = warp * kDRows; r < kTileRows && r0 + r < rows; r += kDThreads / 32 * kDRows) {
+        uint32_t w[kDRows], e[kDRows];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const uint32_t code = w >> (4 * k) & 15u, m = code & 7u;
-            const float d = (float)(m < 4u ? m : m == 4u ? 4u : m == 5u ? 6u : m == 6u ? 8u : 12u);
-            const float f = d * s;
-            out[k] = (uint16_t)((__float_as_uint(f) >> 16) | (code & 8u) << 12);
+        for (int k = 0; k < kDRows; ++k) {
+            const bool in = r0 + r + k < rows;
+            w[k] = in ? __ldg(reinterpret_cast<const uint32_t *>(codes + (size_t)(r0 + r + k) * pitch + c / 2)) : 0u;
+            e[k] = __ldg(sc + scale_at(r + k, b % kTileBlocks));
         }
-        uint16_t *dst = v + (size_t)row * cols + c;
-        if ((cols & 7) == 0) {
-            *reinterpret_cast<uint4 *>(dst) = make_uint4(out[0] | (uint32_t)out[1] << 16, out[2] | (uint32_t)out[3] << 16, out[4] | (uint32_t)out[5] << 16, out[6] | (uint32_t)out[7] << 16);
-        } else {
 #pragma unroll
-            for (int k = 0; k < 8; ++k)
-                if (c + k < cols) dst[k] = out[k];
+        for (int k = 0; k < kDRows; ++k) {
+            if (r0 + r + k >= rows) break;
+            const uint4 o = values4(w[k], e[k]);
+            uint16_t *dst = v + (size_t)(r0 + r + k) * cols + c;
+            if ((cols & 7) == 0) {
+                *reinterpret_cast<uint4 *>(dst) = o;
+            } else {
+                const uint32_t u[4] = {o.x, o.y, o.z, o.w};
+#pragma unroll
+                for (int q = 0; q < 8; ++q)
+                    if (c + q < cols) dst[q] = (uint16_t)(u[q >> 1] >> (16 * (q & 1)));
+            }
         }
     }
 }
@@ -143,15 +170,18 @@ int launch_mxfp4_quantize(const uint16_t *v, int rows, int cols, uint8_t *codes,
     const QuantizeParams p = {v, codes, scales, codes_t, scales_t, rows, cols};
     const dim3 grid((unsigned)((cols + 127) / 128), (unsigned)((rows + 127) / 128));
     if (grid.y > 65535u) return LORDS_ERR_SHAPE;
-    lords_mxfp4_quantize_kernel<<<grid, kQThreads, 0, stream>>>(p);
+    if (codes && codes_t) lords_mxfp4_quantize_kernel<true, true><<<grid, kQThreads, 0, stream>>>(p);
+    else if (codes) lords_mxfp4_quantize_kernel<true, false><<<grid, kQThreads, 0, stream>>>(p);
+    else lords_mxfp4_quantize_kernel<false, true><<<grid, kQThreads, 0, stream>>>(p);
     LORDS_CUDA_TRY(cudaGetLastError());
     return LORDS_OK;
 }
 
 int launch_mxfp4_dequantize(const uint8_t *codes, const uint8_t *scales, int rows, int cols, uint16_t *v, cudaStream_t stream)
 {
-    const dim3 grid((unsigned)((cols + 2047) / 2048), (unsigned)(rows < 65535 ? rows : 65535));
-    lords_mxfp4_dequantize_kernel<<<grid, 256, 0, stream>>>(codes, scales, rows, cols, v);
+    const dim3 grid((unsigned)((cols + 255) / 256), (unsigned)((rows + kTileRows - 1) / kTileRows));
+    if (grid.y > 65535u) return LORDS_ERR_SHAPE;
+    lords_mxfp4_dequantize_kernel<<<grid, kDThreads, 0, stream>>>(codes, scales, rows, cols, v);
     LORDS_CUDA_TRY(cudaGetLastError());
     return LORDS_OK;
 }

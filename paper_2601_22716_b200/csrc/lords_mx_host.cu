@@ -21,7 +21,10 @@ static size_t scales_bytes(int rows, int cols) { return (size_t)((rows + mx::kTi
 
 static bool dims_ok(int64_t rows, int64_t cols) { return rows >= 1 && cols >= 1 && rows <= LORDS_MX_DIM_MAX && cols <= LORDS_MX_DIM_MAX; }
 
-static int product(const MxProblem &p, State &st, cudaStream_t s) { return launch_mxfp4_stream(p, st, s); }
+static int product(const MxProblem &p, State &st, cudaStream_t s)
+{
+    return p.M > 128 ? launch_mxfp4_pair(p, st, s) : launch_mxfp4_stream(p, st, s);
+}
 
 static int matmul_common(const uint8_t *xq, const uint8_t *xs, const uint8_t *w, const uint8_t *ws, int M, int m, int n, void *y, int y_f32, void *stream)
 {

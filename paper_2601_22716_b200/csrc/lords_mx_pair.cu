@@ -1,0 +1,305 @@
+// y = x W^T on microscaled 4-bit operands, for many tokens: tcgen05.mma kind::mxf4 on CTA pairs (cta_group::2).
+//
+// A pair computes 256 tokens x BN out-features; the tokens are the MMA's rows, so that a thread of the epilogue holds one token's
+// neighbouring out-features and stores whole sectors.  A step is 256 columns, 128 bytes of codes a row: each CTA loads its 128
+// tokens and its half of the out-features by TMA, its tokens' scales and the scales of all BN out-features, which go on to TMEM
+// (tcgen05.cp) ahead of the step's four MMAs.  Tiles are dealt out to as many pairs as are resident; with BN = 128 two accumulators take turns, so
+// that a tile's stores run beside the next one's MMAs, with 256 the loads of the next tile do.
+//
+// Bound: 4-bit MMAs (four times the bf16 rate) at BN = 256 against 128 (128 + BN / 2) bytes a step and CTA from L2.
+// No scratch memory.  Every wait is bounded; on expiry the role records LORDS_ERR_TIMEOUT and leaves its loop.
+#include <cuda.h>
+#include <cuda_bf16.h>
+
+#include "lords_internal.h"
+#include "lords_mx.cuh"
+#include "lords_pair.cuh"
+#include "lords_ptx.cuh"
+#include "lords_tc_common.cuh"
+
+namespace lords {
+
+namespace {
+
+using namespace ptx;
+using namespace mx;
+
+constexpr int kPTokens = 256;                // tokens per CTA pair
+constexpr int kPEpiWarp0 = 4;                // warps from 4 on: epilogue; 0: TMA, 1: MMA issuer, 2: TMEM
+
+template <int BN> struct PCfg {
+    static constexpr int EPI = 8;
+    static constexpr int THREADS = (kPEpiWarp0 + EPI) * 32;
+    static constexpr int XTILE = 128 * 128;                      // this CTA's tokens
+    static constexpr int WTILE = BN / 2 * 128;                   // this CTA's half of the out-features
+    static constexpr int XSF = 2 * kTileBytes;                   // scales of a step: two tiles of four blocks
+    static constexpr int WSF = BN / kTileRows * 2 * kTileBytes;
+    static constexpr int STAGE = XTILE + WTILE + XSF + WSF;
+    static constexpr int STAGES = (226 * 1024) / STAGE;
+    static constexpr int SMEM = 1024 + STAGES * STAGE + 256;
+    static constexpr int ACCS = BN <= 128 ? 2 : 1;
+    static constexpr uint32_t SF_COL = ACCS * BN;                // behind the accumulators: two sets of scales of a step
+    static constexpr uint32_t SF_COLS = 8 + BN / kTileRows * 8;
+    static_assert(STAGE % 1024 == 0 && SMEM <= 232448 && SF_COL + 2 * SF_COLS <= 512, "shared memory and TMEM");
+};
+
+struct alignas(64) PairParams {
+    CUtensorMap tm_x;        // bytes [M][pitch], box {128, 128}, 128-byte swizzle (zeros behind the last row and byte)
+    CUtensorMap tm_w;        // bytes [m][pitch], box {128, BN / 2}
+    CUtensorMap tm_xs;       // scale tiles as words [row tiles][128 ktiles], box {256, 1}
+    CUtensorMap tm_ws;       // the same, box {256, BN / 128}
+    int M, m;
+    int tok_tiles, tiles, steps, blocks;
+    int pairs;
+    void *y;
+    int y_f32;
+    int *status;
+};
+
+__device__ __forceinline__ uint32_t pack_bf16(uint32_t lo, uint32_t hi)
+{
+    const __nv_bfloat162 v = __floats2bfloat162_rn(__uint_as_float(lo), __uint_as_float(hi));
+    return *reinterpret_cast<const uint32_t *>(&v);
+}
+__device__ __forceinline__ void store_sector(void *at, const uint32_t *w)
+{
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]),
+                 "r"(w[7])
+                 : "memory");
+}
+
+template <int BN>
+__global__ void __launch_bounds__(PCfg<BN>::THREADS, 1) lords_mxfp4_pair_kernel(const __grid_constant__ PairParams p)
+{
+    using C = PCfg<BN>;
+    constexpr int STAGES = C::STAGES;
+    extern __shared__ uint8_t p_smem[];
+    const uint32_t base = (smem_u32(p_smem) + 1023u) & ~1023u;
+    const uint32_t bars = base + STAGES * C::STAGE;
+    const uint32_t bar_full = bars, bar_empty = bars + 8 * STAGES, bar_acc_full = bar_empty + 8 * STAGES, bar_acc_empty = bar_acc_full + 16;
+    const uint32_t tmem_slot = bar_acc_empty + 16;
+    static_assert(8 * (2 * STAGES + 4) + 4 <= 256, "barrier area");
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int rank = (int)cluster_ctarank(), pair = (int)(blockIdx.x >> 1);
+    const int *status = p.status;
+    bool failed = false;
+
+    if (warp == 0) {
+        if (lane < 2 * STAGES + 2) mbar_init(bars + 8 * lane, 1);
+        if (lane >= 2 * STAGES + 2 && lane < 2 * STAGES + 4) mbar_init(bars + 8 * lane, 2 * C::EPI);       // read by both CTAs' epilogue
+        fence_mbar_init();
+        if (lane == 0) { tma_prefetch_desc(&p.tm_x); tma_prefetch_desc(&p.tm_w); tma_prefetch_desc(&p.tm_xs); tma_prefetch_desc(&p.tm_ws); }
+    } else if (warp == 2) {
+        tmem_alloc2(tmem_slot, 512);
+    }
+    tc_fence_before_sync();
+    __syncthreads();
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");       // both CTAs' barriers exist
+    tc_fence_after_sync();
+    uint32_t tmem_base;
+    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(tmem_base) : "r"(tmem_slot));
+    griddep_launch_dependents();
+    griddep_wait();
+
+    if (warp == 0) {
+        // ------------------------------------------------------------------ TMA
+        if (lane == 0) {
+            const uint32_t full0 = map_to_rank(bar_full, 0);
+            int it = 0;
+            for (int tile = pair; tile < p.tiles && !failed; tile += p.pairs) {
+                const int wt = tile / p.tok_tiles, tt = tile - wt * p.tok_tiles;
+                for (int k = 0; k < p.steps; ++k, ++it) {
+                    const int s = it % STAGES;
+                    if (it >= STAGES && !mbar_wait(bar_empty + 8 * s, (uint32_t)((it / STAGES - 1) & 1), status, 71)) { failed = true; break; }
+                    if (rank == 0) mbar_expect_tx(bar_full + 8 * s, 2u * C::STAGE);
+                    const uint32_t dst = base + (uint32_t)(s * C::STAGE), bar = full0 + 8 * s;
+                    tma_load_2d_pair(dst, &p.tm_x, k * 128, tt * kPTokens + rank * 128, bar);
+                    tma_load_2d_pair(dst + C::XTILE, &p.tm_w, k * 128, wt * BN + rank * (BN / 2), bar);
+                    tma_load_2d_pair(dst + C::XTILE + C::WTILE, &p.tm_xs, k * 256, tt * 2 + rank, bar);
+                    tma_load_2d_pair(dst + C::XTILE + C::WTILE + C::XSF, &p.tm_ws, k * 256, wt * (BN / kTileRows), bar);
+                }
+            }
+            // nothing of this CTA is in flight when it ends: the last round of stages has been read
+            for (int k = it > STAGES ? it - STAGES : 0; k < it && !failed; ++k)
+                if (!mbar_wait(bar_empty + 8 * (k % STAGES), (uint32_t)((k / STAGES) & 1), status, 72)) failed = true;
+        }
+        __syncwarp();
+    } else if (warp == 1 && rank == 0) {
+        // ------------------------------------------------------------------ MMA issuer (the pair's even CTA)
+        const uint32_t hi = (uint32_t)(umma_desc_sw128(0, 1024, 16) >> 32), lo0 = (uint32_t)umma_desc_sw128(0, 1024, 16);
+        const uint32_t tmem_u = warp_uniform(tmem_base), leader = elect_one();
+        int it = 0, n = 0;
+        for (int tile = pair; tile < p.tiles && !failed; tile += p.pairs, ++n) {
+            const int a = n % C::ACCS;
+            if (n >= C::ACCS && !mbar_wait_cluster(bar_acc_empty + 8 * a, (uint32_t)((n / C::ACCS - 1) & 1), status, 73)) { failed = true; break; }
+            tc_fence_after_sync();
+            for (int k = 0; k < p.steps; ++k, ++it) {
+                const int s = it % STAGES;
+                if (!mbar_wait_cluster(bar_full + 8 * s, (uint32_t)((it / STAGES) & 1), status, 74)) { failed = true; break; }
+                tc_fence_after_sync();
+                const uint32_t at = base + (uint32_t)(s * C::STAGE), sx = at + C::XTILE + C::WTILE, sw = sx + C::XSF;
+                const uint32_t a_lo = lo0 | ((at & 0x3FFFFu) >> 4), b_lo = lo0 | (((at + C::XTILE) & 0x3FFFFu) >> 4);
+                const uint32_t cx = tmem_u + C::SF_COL + (uint32_t)((it & 1) * C::SF_COLS), cw = cx + 8;
+                const int mmas = (p.blocks - 8 * k + 1) / 2 < 4 ? (p.blocks - 8 * k + 1) / 2 : 4;
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+                    if (2 * j < mmas) {
+                        scales_to_tmem2(cx + 4 * j, scales_desc(sx + (uint32_t)(j * kTileBytes)), leader);
+                        // (a row of tiles after the other in shared memory, the tiles of a K side by side in TMEM)
+#pragma unroll
+                        for (int r = 0; r < BN / kTileRows; ++r)
+                            scales_to_tmem2(cw + (uint32_t)(j * (BN / 32) + 4 * r), scales_desc(sw + (uint32_t)((2 * r + j) * kTileBytes)), leader);
+                    }
+#pragma unroll
+                for (int kk = 0; kk < 4; ++kk)
+                    if (kk < mmas)
+                        umma2_mxf4_ss(tmem_u + (uint32_t)(a * BN), umma_desc_pack(a_lo + 2 * kk, hi), umma_desc_pack(b_lo + 2 * kk, hi),
+                                      umma_idesc_mxf4(kPTokens, BN, kk & 1), cx + 4 * (kk >> 1), cw + (BN / 32) * (kk >> 1), (k > 0 || kk > 0) ? 1u : 0u, leader);
+                umma2_commit(bar_empty + 8 * s, leader);
+                if (k == p.steps - 1) umma2_commit(bar_acc_full + 8 * a, leader);
+            }
+        }
+    } else if (warp >= kPEpiWarp0) {
+        // ------------------------------------------------------------------ epilogue: lane = token, columns = out-features
+        const int q = warp & 3, ch = (warp - kPEpiWarp0) >> 2;                // quadrant of the tokens, share of the columns
+        constexpr int CW = BN / (C::EPI / 4);
+        const uint32_t empty0 = map_to_rank(bar_acc_empty, 0);
+        const uint32_t acc = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(ch * CW);
+        const size_t row_bytes = (size_t)p.m * (p.y_f32 ? 4 : 2);
+        int n = 0;
+        for (int tile = pair; tile < p.tiles; tile += p.pairs, ++n) {
+            const int a = n % C::ACCS, wt = tile / p.tok_tiles, tt = tile - wt * p.tok_tiles;
+            if (!__all_sync(0xffffffffu, mbar_wait_cluster(bar_acc_full + 8 * a, (uint32_t)((n / C::ACCS) & 1), status, 75))) { failed = true; break; }
+            tc_fence_after_sync();
+            const int t = tt * kPTokens + rank * 128 + q * 32 + lane;
+#pragma unroll 1
+            for (int c0 = 0; c0 < CW; c0 += 32) {
+                uint32_t v[32];
+                tmem_ld_32x32(acc + (uint32_t)(a * BN + c0), v);
+                tmem_wait_ld(v);
+                if (c0 + 32 == CW) {            // the accumulator has been read
+                    tc_fence_before_sync();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_pair(empty0 + 8 * a);
+                }
+                const int i = wt * BN + ch * CW + c0;
+                if (t >= p.M || i >= p.m) continue;
+                if (p.y_f32) {
+                    float *dst = static_cast<float *>(p.y) + (size_t)t * p.m + i;
+                    if (i + 32 <= p.m && (row_bytes & 31) == 0 && (reinterpret_cast<uintptr_t>(p.y) & 31) == 0) {
+#pragma unroll
+                        for (int g = 0; g < 4; ++g) store_sector(dst + 8 * g, v + 8 * g);
+                    } else {
+#pragma unroll
+                        for (int c = 0; c < 32; ++c)
+                            if (i + c < p.m) dst[c] = __uint_as_float(v[c]);
+                    }
+                } else {
+                    uint32_t w[16];
+#pragma unroll
+                    for (int c = 0; c < 16; ++c) w[c] = pack_bf16(v[2 * c], v[2 * c + 1]);
+                    uint16_t *dst = static_cast<uint16_t *>(p.y) + (size_t)t * p.m + i;
+                    if (i + 32 <= p.m && (row_bytes & 31) == 0 && (reinterpret_cast<uintptr_t>(p.y) & 31) == 0) {
+                        store_sector(dst, w);
+                        store_sector(dst + 16, w + 8);
+                    } else {
+#pragma unroll
+                        for (int c = 0; c < 32; ++c)
+                            if (i + c < p.m) dst[c] = (uint16_t)(w[c >> 1] >> (16 * (c & 1)));
+                    }
+                }
+            }
+        }
+    }
+
+    if (failed) ptx::record_give_up(p.status, LORDS_ERR_TIMEOUT);
+    tc_fence_before_sync();
+    __syncthreads();
+    // neither CTA leaves while the other may still signal its barriers or read its operands
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    if (warp == 2) {
+        tc_fence_after_sync();
+        tmem_dealloc2(tmem_base, 512);
+    }
+}
+
+template <int BN> struct PairVariant {
+    static void fill(cudaLaunchConfig_t &cfg, cudaLaunchAttribute *attr, int pairs, cudaStream_t stream)
+    {
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = 2;
+        attr[0].val.clusterDim.y = 1;
+        attr[0].val.clusterDim.z = 1;
+        attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[1].val.programmaticStreamSerializationAllowed = 1;
+        cfg = cudaLaunchConfig_t{};
+        cfg.gridDim = dim3((unsigned)(2 * pairs));
+        cfg.blockDim = dim3(PCfg<BN>::THREADS);
+        cfg.dynamicSmemBytes = PCfg<BN>::SMEM;
+        cfg.stream = stream;
+        cfg.attrs = attr;
+        cfg.numAttrs = 2;
+    }
+    // CTA pairs that can be resident at once
+    static int resident(const State &st)
+    {
+        static int cache[kMaxDevices] = {};
+        const int dev = device_slot(st);
+        if (cache[dev] == 0) {
+            if (cudaFuncSetAttribute(lords_mxfp4_pair_kernel<BN>, cudaFuncAttributeMaxDynamicSharedMemorySize, PCfg<BN>::SMEM) != cudaSuccess) return 0;
+            cudaLaunchConfig_t cfg;
+            cudaLaunchAttribute attr[2];
+            fill(cfg, attr, 1, nullptr);
+            int n = 0;
+            if (cudaOccupancyMaxActiveClusters(&n, lords_mxfp4_pair_kernel<BN>, &cfg) != cudaSuccess) (void)cudaGetLastError();
+            cache[dev] = n >= 1 ? n : -1;
+        }
+        return cache[dev] > 0 ? cache[dev] : 0;
+    }
+};
+
+template <int BN> int run_pair(const MxProblem &p, State &st, cudaStream_t stream)
+{
+    const int resident = PairVariant<BN>::resident(st);
+    if (resident < 1) return LORDS_ERR_UNSUPPORTED;
+    PairParams k;
+    const uint64_t pitch = (uint64_t)codes_pitch(p.n), words = (uint64_t)scale_tiles_of(p.n) * (kTileBytes / 4);
+    const uint64_t xt = (uint64_t)((p.M + kTileRows - 1) / kTileRows), wt = (uint64_t)((p.m + kTileRows - 1) / kTileRows);
+    if (!make_map_2d(&k.tm_x, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, p.xq, pitch, (uint64_t)p.M, 128, 128, CU_TENSOR_MAP_SWIZZLE_128B) ||
+        !make_map_2d(&k.tm_w, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, p.w, pitch, (uint64_t)p.m, 128, BN / 2, CU_TENSOR_MAP_SWIZZLE_128B) ||
+        !make_map_2d(&k.tm_xs, CU_TENSOR_MAP_DATA_TYPE_INT32, 4, p.xs, words, xt, 256, 1, CU_TENSOR_MAP_SWIZZLE_NONE) ||
+        !make_map_2d(&k.tm_ws, CU_TENSOR_MAP_DATA_TYPE_INT32, 4, p.ws, words, wt, 256, BN / kTileRows, CU_TENSOR_MAP_SWIZZLE_NONE))
+        return LORDS_ERR_CUDA;
+    k.M = p.M; k.m = p.m;
+    k.tok_tiles = (p.M + kPTokens - 1) / kPTokens;
+    const long long tiles = (long long)k.tok_tiles * ((p.m + BN - 1) / BN);
+    if (tiles > 2147483647LL - 65536) return LORDS_ERR_SHAPE;
+    k.tiles = (int)tiles;
+    k.steps = (p.n + 255) / 256;
+    k.blocks = blocks_of(p.n);
+    k.pairs = k.tiles < resident ? k.tiles : resident;
+    k.y = p.y; k.y_f32 = p.y_f32;
+    k.status = st.status_word;
+    cudaLaunchConfig_t cfg;
+    cudaLaunchAttribute attr[2];
+    PairVariant<BN>::fill(cfg, attr, k.pairs, stream);
+    LORDS_CUDA_TRY(cudaLaunchKernelEx(&cfg, lords_mxfp4_pair_kernel<BN>, k));
+    st.last_launches += 1;
+    st.last_path = "mxfp4_pair";
+    return LORDS_OK;
+}
+
+}  // namespace
+
+int launch_mxfp4_pair(const MxProblem &p, State &st, cudaStream_t stream)
+{
+    if (p.x) return LORDS_ERR_UNSUPPORTED;
+    const long long tok = (p.M + kPTokens - 1) / kPTokens;
+    // 256 out-features a pair where they fill the pairs' waves as well as 128 do
+    const long long w256 = (tok * ((p.m + 255) / 256) + 73) / 74, w128 = (tok * ((p.m + 127) / 128) + 73) / 74;
+    return 2 * w256 <= w128 ? run_pair<256>(p, st, stream) : run_pair<128>(p, st, stream);
+}
+
+}  // namespace lords
