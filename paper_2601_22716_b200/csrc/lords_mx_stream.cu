@@ -32,20 +32,28 @@ using namespace mx;
 
 constexpr int kRows = 128;                   // rows of W per CTA
 constexpr int kStep = 256;                   // columns a step: 128 bytes of codes
-constexpr int kConvWarp0 = 4;                // warps 4 .. 7: x to 4 bits, then the epilogue; 0: TMA, 1: MMA issuer, 2: TMEM
-constexpr int kSThreads = 256;
+constexpr int kConvWarp0 = 4;                // warps from 4 on: x to 4 bits, then (the first four) the epilogue; 0: TMA, 1: MMA issuer, 2: TMEM
+constexpr int kSplitMax = 8;                 // CTAs that share a tile's steps
+constexpr int kBatch = 8;                    // QX: steps whose slice of x is converted together
+constexpr int kBatches = 2;                  // ... and batches in shared memory
 
-template <int BN> struct SCfg {
+template <int BN, bool QX> struct SCfg {
+    static constexpr int CONV = QX ? 8 : 4;                         // converter and epilogue warps
+    static constexpr int THREADS = (kConvWarp0 + CONV) * 32;
     static constexpr int WTILE = kRows * 128;
     static constexpr int XTILE = BN * 128;
     static constexpr int SF = 2 * kTileBytes;                       // scales of a step: two tiles of four blocks
-    static constexpr int STAGE = WTILE + XTILE + 2 * SF;            // a multiple of 1024 (BN is a multiple of 8)
-    static constexpr int RECV = BN * kRows * 4;                     // partial sums from the cluster
-    static constexpr int STAGES = (230 * 1024 - 2048 - RECV) / STAGE < 10 ? (230 * 1024 - 2048 - RECV) / STAGE : 10;
-    static constexpr int SMEM = 1024 + STAGES * STAGE + RECV + 512;
+    static constexpr int XSTEP = XTILE + SF;                        // x of a step with its scales
+    static constexpr int STAGE = WTILE + SF + (QX ? 0 : XSTEP);
+    static constexpr int XRING = QX ? kBatches * kBatch * XSTEP : 0;
+    // partial sums from the cluster: ceil(groups / split) * split <= groups + split - 1 places of four tokens x 128 rows
+    static constexpr int RECV = (BN / 4 + kSplitMax - 1) * 4 * kRows * 4;
+    static constexpr int ROOM = 232448 - 1024 - 512 - RECV - XRING;
+    static constexpr int STAGES = ROOM / STAGE < 10 ? ROOM / STAGE : 10;
+    static constexpr int SMEM = 1024 + STAGES * STAGE + XRING + RECV + 512;
     static constexpr uint32_t ACC = BN < 32 ? 32 : BN;              // accumulator columns; behind them two sets of scales
     static constexpr uint32_t TMEM = ACC + 32 <= 64 ? 64 : ACC + 32 <= 128 ? 128 : 256;
-    static_assert(SMEM <= 232448 && STAGE % 1024 == 0, "shared memory");
+    static_assert(SMEM <= 232448 && STAGE % 1024 == 0 && XSTEP % 1024 == 0 && STAGES >= 3, "shared memory");
 };
 
 struct alignas(64) StreamParams {
@@ -61,32 +69,98 @@ struct alignas(64) StreamParams {
     int *status;
 };
 
-template <int BN, bool QX>
-__global__ void __launch_bounds__(kSThreads, 1) lords_mxfp4_stream_kernel(const __grid_constant__ StreamParams p)
+// One, two or four sums of a row, asynchronously to a CTA of the cluster; counted in bytes on its barrier.
+template <int GW> __device__ __forceinline__ void send(uint32_t addr, const uint32_t *v, uint32_t bar)
 {
-    using C = SCfg<BN>;
+    if constexpr (GW == 1)
+        asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.b32 [%0], %1, [%2];" ::"r"(addr), "r"(v[0]), "r"(bar) : "memory");
+    else if constexpr (GW == 2)
+        asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v2.b32 [%0], {%1, %2}, [%3];" ::"r"(addr), "r"(v[0]), "r"(v[1]), "r"(bar) : "memory");
+    else
+        asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v4.b32 [%0], {%1, %2, %3, %4}, [%5];" ::"r"(addr), "r"(v[0]), "r"(v[1]), "r"(v[2]),
+                     "r"(v[3]), "r"(bar) : "memory");
+}
+
+// The cluster's sums: tokens in groups of GW, group g to rank g mod cluster; a received value's place is (group / cluster, rank, row).
+template <int BN, int GW>
+__device__ __forceinline__ bool add_up(const StreamParams &p, uint32_t acc, uint32_t recv, uint32_t bar_recv, int rank, int split, int tokens, int tok0, int ri,
+                                       int i, bool failed)
+{
+    const int groups = (tokens + GW - 1) / GW;
+    const uint32_t row_at = recv + (uint32_t)(ri * 4 * GW);
+#pragma unroll
+    for (int c0 = 0; c0 < BN; c0 += 16) {
+        if (c0 >= tokens) break;
+        uint32_t v[16];
+        tmem_ld_32x16(acc + (uint32_t)c0, v);
+        tmem_wait_ld(v);
+#pragma unroll
+        for (int c = 0; c < 16 && (GW == 4 || c == 0); c += GW) {
+            const int g = (c0 + c) / GW;
+            if (g < groups) {
+                const int to = g % split;
+                const uint32_t where = row_at + (uint32_t)(((g / split) * split + rank) * kRows * 4 * GW);
+                if (to == rank) {
+#pragma unroll
+                    for (int k = 0; k < GW; ++k) sts_u32(where + 4 * k, v[c + k]);
+                } else {
+                    send<GW>(map_to_rank(where, (uint32_t)to), v + c, map_to_rank(bar_recv, (uint32_t)to));
+                }
+            }
+        }
+    }
+    if (rank >= groups) return true;
+    if (!__all_sync(0xffffffffu, mbar_wait_cluster(bar_recv, 0, p.status, 65))) return false;
+    for (int g = rank; g < groups && !failed; g += split) {
+        float sum[GW];
+#pragma unroll
+        for (int k = 0; k < GW; ++k) sum[k] = 0.0f;
+        for (int r = 0; r < split; ++r) {
+            const uint32_t from = row_at + (uint32_t)(((g / split) * split + r) * kRows * 4 * GW);
+            if constexpr (GW == 4) {
+                const uint4 u = lds_v4(from);
+                sum[0] += __uint_as_float(u.x); sum[1] += __uint_as_float(u.y); sum[2] += __uint_as_float(u.z); sum[3] += __uint_as_float(u.w);
+            } else {
+#pragma unroll
+                for (int k = 0; k < GW; ++k) sum[k] += __uint_as_float(lds_u32(from + 4 * k));
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < GW; ++k)
+            if (i < p.m && g * GW + k < tokens) store_out(p.y, p.y_f32, (size_t)(tok0 + g * GW + k) * p.m + i, sum[k]);
+    }
+    return true;
+}
+
+template <int BN, bool QX>
+__global__ void __launch_bounds__(SCfg<BN, QX>::THREADS, 1) lords_mxfp4_stream_kernel(const __grid_constant__ StreamParams p)
+{
+    using C = SCfg<BN, QX>;
     constexpr int STAGES = C::STAGES;
     extern __shared__ uint8_t s_smem[];
     const uint32_t base = (smem_u32(s_smem) + 1023u) & ~1023u;
-    const uint32_t recv = base + STAGES * C::STAGE, bars = recv + C::RECV;
-    const uint32_t bar_full = bars, bar_empty = bar_full + 8 * STAGES, bar_acc = bar_empty + 8 * STAGES, bar_recv = bar_acc + 8, tmem_slot = bar_recv + 8;
-    static_assert(16 * STAGES + 24 <= 512, "barrier area");
+    const uint32_t xring = base + STAGES * C::STAGE, recv = xring + C::XRING, bars = recv + C::RECV;
+    const uint32_t bar_full = bars, bar_empty = bar_full + 8 * STAGES, bar_acc = bar_empty + 8 * STAGES, bar_recv = bar_acc + 8;
+    const uint32_t bar_x = bar_recv + 8, bar_x_free = bar_x + 8 * kBatches, tmem_slot = bar_x_free + 8 * kBatches;
+    static_assert(16 * STAGES + 16 + 16 * kBatches + 8 <= 512, "barrier area");
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int rank = (int)cluster_ctarank(), split = (int)cluster_nctarank();
     const int rt = (int)(blockIdx.x / split), row0 = rt * kRows, tok0 = (int)blockIdx.y * BN;
     const int s_a = (int)((long long)p.steps * rank / split), s_b = (int)((long long)p.steps * (rank + 1) / split);
     const int tokens = p.M - tok0 < BN ? p.M - tok0 : BN;
+    const int gw = tokens > 2 ? 4 : tokens;               // tokens that are added up together
     const int *status = p.status;
     bool failed = false;
 
     if (warp == 0) {
         if (lane == 0) {
-            for (int s = 0; s < STAGES; ++s) { mbar_init(bar_full + 8 * s, QX ? 5 : 1); mbar_init(bar_empty + 8 * s, 1); }
+            for (int s = 0; s < STAGES; ++s) { mbar_init(bar_full + 8 * s, 1); mbar_init(bar_empty + 8 * s, 1); }
             mbar_init(bar_acc, 1);
             mbar_init(bar_recv, 1);
+            for (int s = 0; s < kBatches; ++s) { mbar_init(bar_x + 8 * s, C::CONV); mbar_init(bar_x_free + 8 * s, 1); }
             fence_mbar_init();
-            const int own = tokens > rank ? (tokens - rank + split - 1) / split : 0;
-            if (split > 1) mbar_expect_tx(bar_recv, (uint32_t)((split - 1) * own * kRows * 4));
+            const int groups = (tokens + gw - 1) / gw, own = groups > rank ? (groups - rank + split - 1) / split : 0;
+            if (split > 1) mbar_expect_tx(bar_recv, (uint32_t)((split - 1) * own * kRows * 4 * gw));
             tma_prefetch_desc(&p.tm_w);
             if (!QX) tma_prefetch_desc(&p.tm_x);
         }
@@ -114,11 +188,10 @@ __global__ void __launch_bounds__(kSThreads, 1) lords_mxfp4_stream_kernel(const 
                 const int kt = p.ktiles - 2 * st < 2 ? 1 : 2;
                 mbar_expect_tx(bar, (uint32_t)(C::WTILE + kt * kTileBytes + (QX ? 0 : C::XTILE + kt * kTileBytes)));
                 tma_load_2d(dst, &p.tm_w, st * 128, row0, bar);
-                bulk_load(dst + C::WTILE + C::XTILE, p.ws + ((size_t)rt * p.ktiles + 2 * st) * kTileBytes, (uint32_t)(kt * kTileBytes), bar);
+                bulk_load(dst + C::WTILE, p.ws + ((size_t)rt * p.ktiles + 2 * st) * kTileBytes, (uint32_t)(kt * kTileBytes), bar);
                 if (!QX) {
-                    tma_load_2d(dst + C::WTILE, &p.tm_x, st * 128, tok0, bar);
-                    bulk_load(dst + C::WTILE + C::XTILE + C::SF, p.xs + ((size_t)(tok0 / kTileRows) * p.ktiles + 2 * st) * kTileBytes,
-                              (uint32_t)(kt * kTileBytes), bar);
+                    tma_load_2d(dst + C::WTILE + C::SF, &p.tm_x, st * 128, tok0, bar);
+                    bulk_load(dst + C::WTILE + C::SF + C::XTILE, p.xs + ((size_t)(tok0 / kTileRows) * p.ktiles + 2 * st) * kTileBytes, (uint32_t)(kt * kTileBytes), bar);
                 }
             }
         }
@@ -130,11 +203,13 @@ __global__ void __launch_bounds__(kSThreads, 1) lords_mxfp4_stream_kernel(const 
         const uint32_t xcol = QX ? 0u : (uint32_t)(tok0 % kTileRows / 32);      // x's tile of tokens inside its tile of scales
         int it = 0;
         for (int st = s_a; st < s_b; ++st, ++it) {
-            const int s = it % STAGES;
+            const int s = it % STAGES, batch = it / kBatch;
+            if (QX && it % kBatch == 0 && !mbar_wait_warp(bar_x + 8 * (batch % kBatches), (uint32_t)((batch / kBatches) & 1), status, 66)) { failed = true; break; }
             if (!mbar_wait_warp(bar_full + 8 * s, (uint32_t)((it / STAGES) & 1), status, 62)) { failed = true; break; }
             tc_fence_after_sync();
-            const uint32_t at = base + (uint32_t)(s * C::STAGE), sw = at + C::WTILE + C::XTILE, sx = sw + C::SF;
-            const uint32_t a_lo = lo0 | ((at & 0x3FFFFu) >> 4), b_lo = lo0 | (((at + C::WTILE) & 0x3FFFFu) >> 4);
+            const uint32_t at = base + (uint32_t)(s * C::STAGE), sw = at + C::WTILE;
+            const uint32_t xt = QX ? xring + (uint32_t)(it % (kBatch * kBatches) * C::XSTEP) : sw + C::SF, sx = xt + C::XTILE;
+            const uint32_t a_lo = lo0 | ((at & 0x3FFFFu) >> 4), b_lo = lo0 | ((xt & 0x3FFFFu) >> 4);
             const int mmas = (p.blocks - 8 * st + 1) / 2 < 4 ? (p.blocks - 8 * st + 1) / 2 : 4;
             const uint32_t cw = tmem_u + C::ACC + (uint32_t)((it & 1) * 16), cx = cw + 8;
 #pragma unroll
@@ -149,95 +224,98 @@ __global__ void __launch_bounds__(kSThreads, 1) lords_mxfp4_stream_kernel(const 
                     umma_mxf4_ss(tmem_u, umma_desc_pack(a_lo + 2 * k, hi), umma_desc_pack(b_lo + 2 * k, hi), umma_idesc_mxf4(kRows, BN, k & 1), cw + 4 * (k >> 1),
                                  cx + 4 * (k >> 1) + xcol, (it > 0 || k > 0) ? 1u : 0u, leader);
             umma_commit(bar_empty + 8 * s, leader);
+            if (QX && it % kBatch == kBatch - 1) umma_commit(bar_x_free + 8 * (batch % kBatches), leader);
         }
         umma_commit(bar_acc, leader);
     } else if (warp >= kConvWarp0) {
-        const int q = warp - kConvWarp0;
         if constexpr (QX) {
-            // -------------------------------------------------------------- x to 4 bits: a block of a token per thread and step
-            const int t = (tid - kConvWarp0 * 32) >> 3, b = tid & 7;
-            const uint16_t *row = p.x + (size_t)(t < p.M ? t : 0) * p.n;
-            auto load = [&](int st, uint32_t (&w)[16]) {
-                const int c = st * kStep + b * kBlock;
+            // -------------------------------------------------------------- x to 4 bits, a block at a time, a batch of steps after the other.  (Tokens
+            // from M on are columns of the product that nobody reads: whatever their shared memory holds.)
+            auto load = [&](int t, int c, uint32_t (&w)[16]) {
+                const uint16_t *src = p.x + (size_t)t * p.n + c;
 #pragma unroll
                 for (int k = 0; k < 16; ++k) w[k] = 0u;
-                if (t >= p.M || c >= p.n) return;
+                if (c >= p.n) return;
                 if ((p.n & 7) == 0) {
 #pragma unroll
                     for (int k = 0; k < 4; ++k)
                         if (c + 8 * k < p.n) {
-                            const uint4 v = __ldcg(reinterpret_cast<const uint4 *>(row + c) + k);
+                            const uint4 v = __ldcg(reinterpret_cast<const uint4 *>(src) + k);
                             w[4 * k] = v.x; w[4 * k + 1] = v.y; w[4 * k + 2] = v.z; w[4 * k + 3] = v.w;
                         }
                 } else {
 #pragma unroll
                     for (int k = 0; k < 16; ++k) {
-                        const uint32_t lo = c + 2 * k < p.n ? __ldcg(row + c + 2 * k) : 0u, up = c + 2 * k + 1 < p.n ? __ldcg(row + c + 2 * k + 1) : 0u;
+                        const uint32_t lo = c + 2 * k < p.n ? __ldcg(src + 2 * k) : 0u, up = c + 2 * k + 1 < p.n ? __ldcg(src + 2 * k + 1) : 0u;
                         w[k] = lo | up << 16;
                     }
                 }
             };
-            uint32_t w[16], next[16];
-            if (s_a < s_b) load(s_a, w);
-            int it = 0;
-            for (int st = s_a; st < s_b; ++st, ++it) {
-                const int s = it % STAGES;
-                if (st + 1 < s_b) load(st + 1, next);
-                uint32_t top = 0u;
+            const int steps = s_b - s_a;
+            for (int first = 0; first < steps && !failed; first += kBatch) {
+                const int batch = first / kBatch, count = steps - first < kBatch ? steps - first : kBatch;
+                if (batch >= kBatches && !mbar_wait_warp(bar_x_free + 8 * (batch % kBatches), (uint32_t)((batch / kBatches - 1) & 1), status, 63)) { failed = true; break; }
+                const uint32_t to = xring + (uint32_t)((batch % kBatches) * kBatch * C::XSTEP);
+                // block e: token e / (8 count), step and block of the step e % (8 count); two at a time, so that their loads overlap
+                const int all = p.M * 8 * count;
+                for (int e0 = tid - kConvWarp0 * 32; e0 < all; e0 += 2 * C::CONV * 32) {
+                    uint32_t w[2][16];
+                    int t[2], kb[2];
 #pragma unroll
-                for (int k = 0; k < 16; ++k) top = max_magnitudes(top, w[k]);
-                const uint32_t byte = scale_byte<2>(max(top & 0xFFFFu, top >> 16));
-                uint32_t out[4];
+                    for (int h = 0; h < 2; ++h) {
+                        const int e = e0 + h * C::CONV * 32;
+                        t[h] = e / (8 * count);
+                        kb[h] = e - t[h] * 8 * count;
+                        if (e < all) load(t[h], (s_a + first) * kStep + kb[h] * kBlock, w[h]);
+                    }
 #pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    const uint32_t v[4] = {w[4 * g], w[4 * g + 1], w[4 * g + 2], w[4 * g + 3]};
-                    out[g] = to_codes4(v, byte);
+                    for (int h = 0; h < 2; ++h) {
+                        if (e0 + h * C::CONV * 32 >= all) break;
+                        uint32_t top = 0u, out[4];
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) top = max_magnitudes(top, w[h][k]);
+                        const uint32_t byte = scale_byte<2>(max(top & 0xFFFFu, top >> 16));
+#pragma unroll
+                        for (int g = 0; g < 4; ++g) {
+                            const uint32_t v[4] = {w[h][4 * g], w[h][4 * g + 1], w[h][4 * g + 2], w[h][4 * g + 3]};
+                            out[g] = to_codes4(v, byte);
+                        }
+                        const int b = kb[h] & 7;
+                        const uint32_t at = to + (uint32_t)((kb[h] >> 3) * C::XSTEP);
+                        sts_v4(at + (uint32_t)(t[h] * 128 + ((b ^ (t[h] & 7)) << 4)), make_uint4(out[0], out[1], out[2], out[3]));
+                        asm volatile("st.shared.u8 [%0], %1;" ::"r"(at + C::XTILE + (uint32_t)(b / kTileBlocks * kTileBytes + scale_at(t[h], b % kTileBlocks))), "r"(byte)
+                                     : "memory");
+                    }
                 }
-                if (it >= STAGES && !mbar_wait_warp(bar_empty + 8 * s, (uint32_t)((it / STAGES - 1) & 1), status, 63)) { failed = true; break; }
-                const uint32_t at = base + (uint32_t)(s * C::STAGE) + C::WTILE;
-                if (t < BN) sts_v4(at + (uint32_t)(t * 128 + ((b ^ (t & 7)) << 4)), make_uint4(out[0], out[1], out[2], out[3]));
-                asm volatile("st.shared.u8 [%0], %1;" ::"r"(at + C::XTILE + C::SF + (uint32_t)(b / kTileBlocks * kTileBytes + scale_at(t, b % kTileBlocks))), "r"(byte)
-                             : "memory");
                 fence_proxy_async_smem();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(bar_full + 8 * s);
-#pragma unroll
-                for (int k = 0; k < 16; ++k) w[k] = next[k];
+                if (lane == 0) mbar_arrive(bar_x + 8 * (batch % kBatches));
             }
         }
         // ------------------------------------------------------------------ epilogue: lane = row of W, columns = tokens
-        if (!mbar_wait_warp(bar_acc, 0, status, 64)) failed = true;
-        tc_fence_after_sync();
-        const int ri = q * 32 + lane, i = row0 + ri;
-        const uint32_t acc = tmem_base + ((uint32_t)(q * 32) << 16);
         if (split > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+        const int q = warp & 3;
+        if (warp < kConvWarp0 + 4) {
+            if (!mbar_wait_warp(bar_acc, 0, status, 64)) failed = true;
+            tc_fence_after_sync();
+            const int ri = q * 32 + lane, i = row0 + ri;
+            const uint32_t acc = tmem_base + ((uint32_t)(q * 32) << 16);
+            if (split > 1) {
+                const bool ok = gw == 4   ? add_up<BN, 4>(p, acc, recv, bar_recv, rank, split, tokens, tok0, ri, i, failed)
+                                : gw == 2 ? add_up<BN, 2>(p, acc, recv, bar_recv, rank, split, tokens, tok0, ri, i, failed)
+                                          : add_up<BN, 1>(p, acc, recv, bar_recv, rank, split, tokens, tok0, ri, i, failed);
+                failed = failed || !ok;
+            } else if (!failed) {
+#pragma unroll 1
+                for (int c0 = 0; c0 < tokens; c0 += 16) {
+                    uint32_t v[16];
+                    tmem_ld_32x16(acc + (uint32_t)c0, v);
+                    tmem_wait_ld(v);
+                    if (i < p.m)
 #pragma unroll
-        for (int c0 = 0; c0 < BN; c0 += 16) {
-            if (c0 >= tokens) break;
-            uint32_t v[16];
-            tmem_ld_32x16(acc + (uint32_t)c0, v);
-            tmem_wait_ld(v);
-#pragma unroll
-            for (int c = 0; c < 16; ++c) {
-                const int t = c0 + c;
-                if (t >= tokens) break;
-                if (split == 1) {
-                    if (i < p.m && !failed) store_out(p.y, p.y_f32, (size_t)(tok0 + t) * p.m + i, __uint_as_float(v[c]));
-                    continue;
+                        for (int c = 0; c < 16; ++c)
+                            if (c0 + c < tokens) store_out(p.y, p.y_f32, (size_t)(tok0 + c0 + c) * p.m + i, __uint_as_float(v[c]));
                 }
-                // partial sums lie by slot (token / cluster), rank and row
-                const int to = t % split;
-                const uint32_t where = recv + (uint32_t)((((t / split) * split + rank) * kRows + ri) * 4);
-                if (to == rank) sts_u32(where, v[c]);
-                else st_async_cluster_f32(map_to_rank(where, (uint32_t)to), __uint_as_float(v[c]), map_to_rank(bar_recv, (uint32_t)to));
-            }
-        }
-        if (split > 1 && rank < tokens) {
-            if (!__all_sync(0xffffffffu, mbar_wait_cluster(bar_recv, 0, status, 65))) failed = true;
-            for (int t = rank; t < tokens && !failed; t += split) {
-                float sum = 0.0f;
-                for (int r = 0; r < split; ++r) sum += __uint_as_float(lds_u32(recv + (uint32_t)((((t / split) * split + r) * kRows + ri) * 4)));
-                if (i < p.m) store_out(p.y, p.y_f32, (size_t)(tok0 + t) * p.m + i, sum);
             }
         }
     }
@@ -252,41 +330,67 @@ __global__ void __launch_bounds__(kSThreads, 1) lords_mxfp4_stream_kernel(const 
     }
 }
 
-template <int BN, bool QX> int launch_variant(StreamParams &k, int split, const State &st, cudaStream_t stream)
-{
-    static bool done[kMaxDevices] = {};
-    const int dev = device_slot(st);
-    if (!done[dev]) {
-        LORDS_CUDA_TRY(cudaFuncSetAttribute(lords_mxfp4_stream_kernel<BN, QX>, cudaFuncAttributeMaxDynamicSharedMemorySize, SCfg<BN>::SMEM));
-        done[dev] = true;
+template <int BN, bool QX> struct StreamVariant {
+    using C = SCfg<BN, QX>;
+    static void fill(cudaLaunchConfig_t &cfg, cudaLaunchAttribute *attr, int row_tiles, int tok_tiles, int split, cudaStream_t stream)
+    {
+        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[0].val.programmaticStreamSerializationAllowed = 1;
+        attr[1].id = cudaLaunchAttributeClusterDimension;
+        attr[1].val.clusterDim.x = (unsigned)split;
+        attr[1].val.clusterDim.y = 1;
+        attr[1].val.clusterDim.z = 1;
+        cfg = cudaLaunchConfig_t{};
+        cfg.gridDim = dim3((unsigned)(row_tiles * split), (unsigned)tok_tiles);
+        cfg.blockDim = dim3(C::THREADS);
+        cfg.dynamicSmemBytes = C::SMEM;
+        cfg.stream = stream;
+        cfg.attrs = attr;
+        cfg.numAttrs = 2;
     }
-    const int row_tiles = (k.m + kRows - 1) / kRows, tok_tiles = (k.M + BN - 1) / BN;
-    if (tok_tiles > 65535 || (long long)row_tiles * split > 2147483647LL) return LORDS_ERR_SHAPE;
-    cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = (unsigned)split;
-    attr[1].val.clusterDim.y = 1;
-    attr[1].val.clusterDim.z = 1;
-    cudaLaunchConfig_t cfg = cudaLaunchConfig_t{};
-    cfg.gridDim = dim3((unsigned)(row_tiles * split), (unsigned)tok_tiles);
-    cfg.blockDim = dim3(kSThreads);
-    cfg.dynamicSmemBytes = SCfg<BN>::SMEM;
-    cfg.stream = stream;
-    cfg.attrs = attr;
-    cfg.numAttrs = 2;
-    LORDS_CUDA_TRY(cudaLaunchKernelEx(&cfg, lords_mxfp4_stream_kernel<BN, QX>, k));
-    return LORDS_OK;
-}
-
-// CTAs that share a row tile's steps: as many as SMs allow, at most eight and four steps at least to each.
-int choose_split(int tiles, int steps, int sms)
-{
-    int c = 1;
-    while (c < 8 && tiles * c * 2 <= sms && steps >= 4 * c * 2) c *= 2;
-    return c;
-}
+    // Clusters of `split` CTAs that can be resident at once.
+    static int resident(int split, const State &st)
+    {
+        static int cache[kMaxDevices][kSplitMax + 1] = {};
+        int &c = cache[device_slot(st)][split];
+        if (c == 0) {
+            c = -1;
+            if (cudaFuncSetAttribute(lords_mxfp4_stream_kernel<BN, QX>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM) != cudaSuccess) return 0;
+            cudaLaunchConfig_t cfg;
+            cudaLaunchAttribute attr[2];
+            fill(cfg, attr, 1, 1, split, nullptr);
+            int n = 0;
+            if (cudaOccupancyMaxActiveClusters(&n, lords_mxfp4_stream_kernel<BN, QX>, &cfg) != cudaSuccess) (void)cudaGetLastError();
+            if (n >= 1) c = n;
+        }
+        return c > 0 ? c : 0;
+    }
+    // CTAs that share a tile's steps: the least waves x (steps of a CTA + a fixed part worth four).
+    static int choose_split(int tiles, int steps, const State &st)
+    {
+        int best = 0;
+        long long least = 0;
+        for (int c = 1; c <= kSplitMax && (c == 1 || 2 * c <= steps); ++c) {
+            const int n = resident(c, st);
+            if (n < 1) continue;
+            const long long t = (long long)((tiles + n - 1) / n) * ((steps + c - 1) / c + 4);
+            if (best == 0 || t < least) { best = c; least = t; }
+        }
+        return best;
+    }
+    static int launch(StreamParams &k, const State &st, cudaStream_t stream)
+    {
+        const int row_tiles = (k.m + kRows - 1) / kRows, tok_tiles = (k.M + BN - 1) / BN;
+        const int split = choose_split(row_tiles * tok_tiles, k.steps, st);
+        if (split < 1) return LORDS_ERR_UNSUPPORTED;
+        if (tok_tiles > 65535) return LORDS_ERR_SHAPE;
+        cudaLaunchConfig_t cfg;
+        cudaLaunchAttribute attr[2];
+        fill(cfg, attr, row_tiles, tok_tiles, split, stream);
+        LORDS_CUDA_TRY(cudaLaunchKernelEx(&cfg, lords_mxfp4_stream_kernel<BN, QX>, k));
+        return LORDS_OK;
+    }
+};
 
 }  // namespace
 
@@ -307,13 +411,12 @@ int launch_mxfp4_stream(const MxProblem &p, State &st, cudaStream_t stream)
     if (!make_map_2d(&k.tm_w, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, p.w, pitch, (uint64_t)p.m, 128, kRows, CU_TENSOR_MAP_SWIZZLE_128B)) return LORDS_ERR_CUDA;
     if (qx) k.tm_x = k.tm_w;
     else if (!make_map_2d(&k.tm_x, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, p.xq, pitch, (uint64_t)p.M, 128, (uint32_t)bn, CU_TENSOR_MAP_SWIZZLE_128B)) return LORDS_ERR_CUDA;
-    const int split = choose_split((p.m + kRows - 1) / kRows * ((p.M + bn - 1) / bn), k.steps, st.sm_count);
     int rc;
-    if (qx) rc = launch_variant<16, true>(k, split, st, stream);
-    else if (bn == 16) rc = launch_variant<16, false>(k, split, st, stream);
-    else if (bn == 32) rc = launch_variant<32, false>(k, split, st, stream);
-    else if (bn == 64) rc = launch_variant<64, false>(k, split, st, stream);
-    else rc = launch_variant<128, false>(k, split, st, stream);
+    if (qx) rc = StreamVariant<16, true>::launch(k, st, stream);
+    else if (bn == 16) rc = StreamVariant<16, false>::launch(k, st, stream);
+    else if (bn == 32) rc = StreamVariant<32, false>::launch(k, st, stream);
+    else if (bn == 64) rc = StreamVariant<64, false>::launch(k, st, stream);
+    else rc = StreamVariant<128, false>::launch(k, st, stream);
     if (rc != LORDS_OK) return rc;
     st.last_launches += 1;
     st.last_path = "mxfp4_stream";
