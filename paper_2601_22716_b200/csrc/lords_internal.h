@@ -167,6 +167,6 @@ int launch_mxfp4_pair(const MxProblem &p, State &st, cudaStream_t stream);
 
 // 8-bit checkpoints: rows of whole blocks, and scales four bytes per 128 columns.
 int launch_checkpoint_store(const uint16_t *x, int M, int n, uint8_t *q, uint8_t *e, cudaStream_t stream);
-int launch_checkpoint_load(const uint8_t *q, const uint8_t *e, int M, int n, uint16_t *x, int pitch, cudaStream_t stream);
+int launch_checkpoint_load(const uint8_t *q, const uint8_t *e, int M, int n, uint16_t *x, cudaStream_t stream);
 
 }  // namespace lords

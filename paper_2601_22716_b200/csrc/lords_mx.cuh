@@ -11,6 +11,7 @@
 #include <stdint.h>
 
 #include "lords_ptx.cuh"
+#include "lords_tc_common.cuh"
 
 namespace lords {
 namespace mx {
@@ -27,8 +28,49 @@ __host__ __device__ inline size_t codes_pitch(int cols) { return (size_t)blocks_
 // Where the scale of row i and block b of a tile lies inside it: four words a lane, a word the four blocks of row 32 j + lane.
 __host__ __device__ inline int scale_at(int i, int b) { return (i & 31) * 16 + (i >> 5) * 4 + b; }
 
-// The larger of two pairs of bf16 magnitudes.  As whole numbers they are in order, infinities and NaNs above all others.
-__device__ __forceinline__ uint32_t max_magnitudes(uint32_t top, uint32_t pair) { return __vmaxu2(top, pair & 0x7FFF7FFFu); }
+// The larger magnitudes of two pairs of bf16 values; a NaN in either stays one.
+__device__ __forceinline__ uint32_t max_magnitudes(uint32_t a, uint32_t b)
+{
+    uint32_t d;
+    asm("{\n.reg .b32 u, v;\nabs.bf16x2 u, %1;\nabs.bf16x2 v, %2;\nmax.NaN.bf16x2 %0, u, v;\n}\n" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+__device__ __forceinline__ uint32_t bf16x2_mul(uint32_t a, uint32_t b)
+{
+    uint32_t d;
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+
+// Eight values of a row of `cols` from column c (below cols) on, as pairs, zeros behind the last.  `end`: behind the matrix.
+__device__ __forceinline__ void load8(const uint16_t *__restrict__ row, int cols, int c, const uint16_t *end, uint32_t (&w)[4])
+{
+    const uint16_t *src = row + c;
+    if ((cols & 7) == 0) {
+        const uint4 q = __ldg(reinterpret_cast<const uint4 *>(src));
+        w[0] = q.x; w[1] = q.y; w[2] = q.z; w[3] = q.w;
+        return;
+    }
+    load_words_anywhere<4>(reinterpret_cast<const uint8_t *>(src), reinterpret_cast<const uint8_t *>(end), w);
+    const int left = cols - c;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) w[k] = left >= 2 * k + 2 ? w[k] : left > 2 * k ? w[k] & 0xFFFFu : 0u;
+}
+// ... and to a row.
+__device__ __forceinline__ void store8(uint16_t *row, int cols, int c, uint4 v)
+{
+    uint16_t *dst = row + c;
+    const uint32_t u[4] = {v.x, v.y, v.z, v.w};
+    if ((cols & 7) == 0) {
+        *reinterpret_cast<uint4 *>(dst) = v;
+    } else if (cols - c >= 8) {
+        store_words_anywhere<4>(reinterpret_cast<uint8_t *>(dst), u);
+    } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (c + k < cols) dst[k] = (uint16_t)(u[k >> 1] >> (16 * (k & 1)));
+    }
+}
 
 // Scale byte from the bf16 pattern of the block's largest magnitude; BELOW: 2 for the 4-bit, 0 for the 8-bit format.
 template <int BELOW> __device__ __forceinline__ uint32_t scale_byte(uint32_t top)
@@ -36,20 +78,25 @@ template <int BELOW> __device__ __forceinline__ uint32_t scale_byte(uint32_t top
     const uint32_t ex = top >> 7;
     return ex == 255u ? 255u : ex > (uint32_t)BELOW ? ex - (uint32_t)BELOW : 0u;
 }
-// 2^-E (zero for a block that is not finite: every code is 0 there)
-__device__ __forceinline__ float inverse_scale(uint32_t byte)
+// 2^-E as a pair of bf16 numbers (zero for a block that is not finite: every code is 0 there).  E = 127 (8 bits only): 2^-127, a subnormal number.
+__device__ __forceinline__ uint32_t inverse_scale(uint32_t byte)
 {
-    return byte == 255u ? 0.0f : byte == 254u ? __uint_as_float(0x00400000u) : __uint_as_float((254u - byte) << 23);
+    const uint32_t s = byte == 255u ? 0u : byte == 254u ? 0x0040u : (254u - byte) << 7;
+    return s | s << 16;
 }
 
-// Eight bf16 values (pairs, low half first), times 2^-E, to eight 4-bit codes, low nibble first.
-__device__ __forceinline__ uint32_t to_codes4(const uint32_t (&w)[4], float inv)
+// Eight bf16 values (pairs, low half first) to eight 4-bit codes, low nibble first.  The product with 2^-E is exact: what falls out of bf16's range
+// below is far from the least code.  (Infinities and NaNs times the zero that stands for 2^-E of such a block are NaN, which the
+// conversion makes 6: zeroed at the end.)
+__device__ __forceinline__ uint32_t to_codes4(const uint32_t (&w)[4], uint32_t byte)
 {
+    const uint32_t inv = inverse_scale(byte);
     float v[8];
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-        v[2 * k] = __uint_as_float(w[k] << 16) * inv;
-        v[2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u) * inv;
+        const uint32_t u = bf16x2_mul(w[k], inv);
+        v[2 * k] = __uint_as_float(u << 16);
+        v[2 * k + 1] = __uint_as_float(u & 0xFFFF0000u);
     }
     uint32_t c;
     asm("{\n"
@@ -62,12 +109,6 @@ __device__ __forceinline__ uint32_t to_codes4(const uint32_t (&w)[4], float inv)
         "}\n"
         : "=r"(c)
         : "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]));
-    return c;
-}
-// (infinity and NaN times the zero that stands for 2^-E of such a block are NaN, which the conversion makes 6)
-__device__ __forceinline__ uint32_t to_codes4(const uint32_t (&w)[4], uint32_t byte)
-{
-    const uint32_t c = to_codes4(w, inverse_scale(byte));
     return byte == 255u ? 0u : c;
 }
 

@@ -14,29 +14,13 @@ namespace {
 using namespace mx;
 
 // ------------------------------------------------------------------------------------------------ to 4 bits
-// A CTA takes 128 rows x 128 columns: one whole tile of scales in either orientation.  Along the rows, four neighbouring threads hold a block in
-// registers.  Along the columns, a thread reads two columns x 32 rows back from shared memory.
+// A CTA takes ROWS rows x 128 columns.  Along the rows, four neighbouring threads hold a block in registers.  Along the columns, a thread reads
+// two columns x 32 rows back from shared memory.  Scales meet in shared memory as words of four blocks.
+#ifndef QROWS
+#define QROWS 64
+#endif
 constexpr int kQThreads = 256;
 constexpr int kQPitch = 128 * 2 + 16;       // bytes per row of the tile in shared memory; 16-byte words stay aligned
-
-// Eight values of row i from column c on as pairs, zeros outside the matrix.
-__device__ __forceinline__ void load8(const uint16_t *__restrict__ v, int rows, int cols, int i, int c, uint32_t (&w)[4])
-{
-#pragma unroll
-    for (int k = 0; k < 4; ++k) w[k] = 0u;
-    if (i >= rows || c >= cols) return;
-    const uint16_t *src = v + (size_t)i * cols + c;
-    if ((cols & 7) == 0) {
-        const uint4 q = __ldg(reinterpret_cast<const uint4 *>(src));
-        w[0] = q.x; w[1] = q.y; w[2] = q.z; w[3] = q.w;
-    } else {
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const uint32_t lo = c + 2 * k < cols ? __ldg(src + 2 * k) : 0u, hi = c + 2 * k + 1 < cols ? __ldg(src + 2 * k + 1) : 0u;
-            w[k] = lo | hi << 16;
-        }
-    }
-}
 
 struct QuantizeParams {
     const uint16_t *v;       // bf16 [rows][cols]
@@ -45,75 +29,83 @@ struct QuantizeParams {
     int rows, cols;
 };
 
-template <bool ALONG, bool ACROSS> __global__ void __launch_bounds__(kQThreads) lords_mxfp4_quantize_kernel(const QuantizeParams p)
+template <int ROWS, bool ALONG, bool ACROSS> __global__ void __launch_bounds__(kQThreads) lords_mxfp4_quantize_kernel(const QuantizeParams p)
 {
-    __shared__ __align__(16) uint8_t tile[ACROSS ? 128 * kQPitch : 16];
-    __shared__ __align__(16) uint8_t sc[kTileBytes], sct[kTileBytes];
-    const int tid = threadIdx.x, r0 = (int)blockIdx.y * 128, c0 = (int)blockIdx.x * 128;
-    const int seg = tid & 15, row_in = tid >> 4;
-    uint32_t w[8][4];
+    constexpr int PER = ROWS / 16;          // rows a thread loads eight values of
+    __shared__ __align__(16) uint8_t tile[ACROSS ? ROWS * kQPitch : 16];
+    __shared__ __align__(16) uint8_t sc[ROWS * 4], sct[kTileBytes];
+    const int tid = threadIdx.x, r0 = (int)blockIdx.y * ROWS, c0 = (int)blockIdx.x * 128;
+    const int seg = tid & 15, row_in = tid >> 4, c = c0 + seg * 8;
+    const uint16_t *end = p.v + (size_t)p.rows * p.cols;
+    uint32_t w[PER][4];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) load8(p.v, p.rows, p.cols, r0 + k * 16 + row_in, c0 + seg * 8, w[k]);
+    for (int k = 0; k < PER; ++k) {
+        const int i = r0 + k * 16 + row_in;
+        w[k][0] = w[k][1] = w[k][2] = w[k][3] = 0u;
+        if (i < p.rows && c < p.cols) load8(p.v + (size_t)i * p.cols, p.cols, c, end, w[k]);
+    }
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
+    for (int k = 0; k < PER; ++k) {
         const int rl = k * 16 + row_in;
         if constexpr (ACROSS) *reinterpret_cast<uint4 *>(tile + rl * kQPitch + seg * 16) = make_uint4(w[k][0], w[k][1], w[k][2], w[k][3]);
         if constexpr (ALONG) {
-            uint32_t top = max_magnitudes(max_magnitudes(max_magnitudes(max_magnitudes(0u, w[k][0]), w[k][1]), w[k][2]), w[k][3]);
-            top = __vmaxu2(top, __shfl_xor_sync(0xffffffffu, top, 1));
-            top = __vmaxu2(top, __shfl_xor_sync(0xffffffffu, top, 2));
+            uint32_t top = max_magnitudes(max_magnitudes(w[k][0], w[k][1]), max_magnitudes(w[k][2], w[k][3]));
+            top = max_magnitudes(top, __shfl_xor_sync(0xffffffffu, top, 1));
+            top = max_magnitudes(top, __shfl_xor_sync(0xffffffffu, top, 2));
             const uint32_t byte = scale_byte<2>(max(top & 0xFFFFu, top >> 16));
-            const int c = c0 + seg * 8;
             if (r0 + rl < p.rows && c < (int)codes_pitch(p.cols) * 2)
                 *reinterpret_cast<uint32_t *>(p.codes + (size_t)(r0 + rl) * codes_pitch(p.cols) + c / 2) = to_codes4(w[k], byte);
-            if ((seg & 3) == 0) sc[scale_at(rl, seg >> 2)] = (uint8_t)byte;
+            if ((seg & 3) == 0) sc[rl * 4 + (seg >> 2)] = (uint8_t)byte;
         }
     }
     __syncthreads();
-    if (ALONG && tid < kTileBytes / 16)
-        reinterpret_cast<uint4 *>(p.scales + ((size_t)blockIdx.y * scale_tiles_of(p.cols) + blockIdx.x) * kTileBytes)[tid] = reinterpret_cast<const uint4 *>(sc)[tid];
-    if constexpr (!ACROSS) return;
-    {
-        const int pair = tid & 63, b = tid >> 6;        // two columns, a block of 32 rows
-        uint32_t u[32];
-        uint32_t top = 0u;
+    // a row's four scales are a word of the tile of scales; the rows behind the last are part of it
+    if (ALONG && tid < ROWS) {
+        const int i = r0 + tid;
+        *reinterpret_cast<uint32_t *>(p.scales + ((size_t)(i / kTileRows) * scale_tiles_of(p.cols) + blockIdx.x) * kTileBytes + scale_at(i % kTileRows, 0)) =
+            *reinterpret_cast<const uint32_t *>(sc + tid * 4);
+    }
+    if constexpr (ACROSS) {
+        for (int e = tid; e < 64 * (ROWS / 32); e += kQThreads) {
+            const int pair = e & 63, b = e >> 6;        // two columns, a block of 32 rows
+            uint32_t u[32];
+            uint32_t top = 0u;
 #pragma unroll
-        for (int k = 0; k < 32; ++k) {
-            u[k] = *reinterpret_cast<const uint32_t *>(tile + (b * 32 + k) * kQPitch + pair * 4);
-            top = max_magnitudes(top, u[k]);
-        }
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const uint32_t byte = scale_byte<2>(h ? top >> 16 : top & 0xFFFFu);
-            uint32_t out[4];
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                uint32_t x[4];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) x[k] = __byte_perm(u[8 * g + 2 * k], u[8 * g + 2 * k + 1], h ? 0x7632 : 0x5410);
-                out[g] = to_codes4(x, byte);
+            for (int k = 0; k < 32; ++k) {
+                u[k] = *reinterpret_cast<const uint32_t *>(tile + (b * 32 + k) * kQPitch + pair * 4);
+                top = max_magnitudes(top, u[k]);
             }
-            const int col = c0 + 2 * pair + h, r = r0 + b * 32;
-            if (col < p.cols && r < p.rows)
-                *reinterpret_cast<uint4 *>(p.codes_t + (size_t)col * codes_pitch(p.rows) + r / 2) = make_uint4(out[0], out[1], out[2], out[3]);
-            sct[scale_at(2 * pair + h, b)] = (uint8_t)byte;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const uint32_t byte = scale_byte<2>(h ? top >> 16 : top & 0xFFFFu);
+                uint32_t out[4];
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    uint32_t x[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) x[k] = __byte_perm(u[8 * g + 2 * k], u[8 * g + 2 * k + 1], h ? 0x7632 : 0x5410);
+                    out[g] = to_codes4(x, byte);
+                }
+                const int col = c0 + 2 * pair + h, r = r0 + b * 32;
+                if (col < p.cols && r < p.rows)
+                    *reinterpret_cast<uint4 *>(p.codes_t + (size_t)col * codes_pitch(p.rows) + r / 2) = make_uint4(out[0], out[1], out[2], out[3]);
+                sct[(2 * pair + h) * (ROWS / 32) + b] = (uint8_t)byte;
+            }
+        }
+        __syncthreads();
+        // a column's scales of this CTA's rows are a part of a word (the whole of it with 128 rows)
+        if (tid < 128) {
+            uint8_t *dst = p.scales_t + ((size_t)blockIdx.x * scale_tiles_of(p.rows) + r0 / 128) * kTileBytes + scale_at(tid, r0 % 128 / 32);
+            if constexpr (ROWS == 128) *reinterpret_cast<uint32_t *>(dst) = *reinterpret_cast<const uint32_t *>(sct + tid * 4);
+            else *reinterpret_cast<uint16_t *>(dst) = *reinterpret_cast<const uint16_t *>(sct + tid * 2);
         }
     }
-    __syncthreads();
-    if (tid < kTileBytes / 16)
-        reinterpret_cast<uint4 *>(p.scales_t + ((size_t)blockIdx.x * scale_tiles_of(p.rows) + blockIdx.y) * kTileBytes)[tid] = reinterpret_cast<const uint4 *>(sct)[tid];
 }
 
 // ----------------------------------------------------------------------------------------------- from 4 bits
 // A code's three low bits are a bf16 exponent's last two bits and the first of its mantissa, less 126 in the exponent: moved there and multiplied by 2^126,
 // and by 2^E then, both exactly (zero and a half too, as a subnormal number times 2^126).  Two codes at a time; the word's nibbles k and
 // k + 4 are taken together.
-__device__ __forceinline__ uint32_t bf16x2_mul(uint32_t a, uint32_t b)
-{
-    uint32_t d;
-    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
-    return d;
-}
 __device__ __forceinline__ uint4 values4(uint32_t w, uint32_t byte)
 {
     // 2^E as a bf16 number: 2^-127 is subnormal, and the pattern of a NaN stands for 255
@@ -149,30 +141,25 @@ __global__ void __launch_bounds__(kDThreads) lords_mxfp4_dequantize_kernel(const
 #pragma unroll
         for (int k = 0; k < kDRows; ++k) {
             if (r0 + r + k >= rows) break;
-            const uint4 o = values4(w[k], e[k]);
-            uint16_t *dst = v + (size_t)(r0 + r + k) * cols + c;
-            if ((cols & 7) == 0) {
-                *reinterpret_cast<uint4 *>(dst) = o;
-            } else {
-                const uint32_t u[4] = {o.x, o.y, o.z, o.w};
-#pragma unroll
-                for (int q = 0; q < 8; ++q)
-                    if (c + q < cols) dst[q] = (uint16_t)(u[q >> 1] >> (16 * (q & 1)));
-            }
+            store8(v + (size_t)(r0 + r + k) * cols, cols, c, values4(w[k], e[k]));
         }
     }
 }
 
 }  // namespace
 
+template <int ROWS> static void launch_quantize_rows(const QuantizeParams &p, cudaStream_t stream)
+{
+    // (whole tiles of scales are written, the rows behind the last among them)
+    const dim3 grid((unsigned)((p.cols + 127) / 128), (unsigned)((p.rows + 127) / 128 * (128 / ROWS)));
+    if (p.codes && p.codes_t) lords_mxfp4_quantize_kernel<ROWS, true, true><<<grid, kQThreads, 0, stream>>>(p);
+    else if (p.codes) lords_mxfp4_quantize_kernel<ROWS, true, false><<<grid, kQThreads, 0, stream>>>(p);
+    else lords_mxfp4_quantize_kernel<ROWS, false, true><<<grid, kQThreads, 0, stream>>>(p);
+}
+
 int launch_mxfp4_quantize(const uint16_t *v, int rows, int cols, uint8_t *codes, uint8_t *scales, uint8_t *codes_t, uint8_t *scales_t, cudaStream_t stream)
 {
-    const QuantizeParams p = {v, codes, scales, codes_t, scales_t, rows, cols};
-    const dim3 grid((unsigned)((cols + 127) / 128), (unsigned)((rows + 127) / 128));
-    if (grid.y > 65535u) return LORDS_ERR_SHAPE;
-    if (codes && codes_t) lords_mxfp4_quantize_kernel<true, true><<<grid, kQThreads, 0, stream>>>(p);
-    else if (codes) lords_mxfp4_quantize_kernel<true, false><<<grid, kQThreads, 0, stream>>>(p);
-    else lords_mxfp4_quantize_kernel<false, true><<<grid, kQThreads, 0, stream>>>(p);
+    launch_quantize_rows<QROWS>({v, codes, scales, codes_t, scales_t, rows, cols}, stream);
     LORDS_CUDA_TRY(cudaGetLastError());
     return LORDS_OK;
 }

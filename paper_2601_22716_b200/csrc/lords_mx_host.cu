@@ -73,7 +73,7 @@ template <class Call> static int with_values(const uint8_t *q, const uint8_t *e,
     State rest = st;
     rest.workspace_bytes = (st.workspace_bytes - bytes) & ~(size_t)255;
     uint16_t *x = reinterpret_cast<uint16_t *>(st.workspace + rest.workspace_bytes);
-    int rc = launch_checkpoint_load(q, e, M, n, x, n, stream);
+    int rc = launch_checkpoint_load(q, e, M, n, x, stream);
     if (rc == LORDS_OK) rc = call(x, rest);
     if (rc != LORDS_OK) return rc;
     st.last_launches = rest.last_launches + 1;
@@ -194,7 +194,7 @@ int lords_checkpoint_load(const uint8_t *q, const uint8_t *e, int M, int n, void
     int rc = ready();
     if (rc != LORDS_OK) return rc;
     State &st = state();
-    rc = launch_checkpoint_load(q, e, M, n, static_cast<uint16_t *>(x), n, static_cast<cudaStream_t>(stream));
+    rc = launch_checkpoint_load(q, e, M, n, static_cast<uint16_t *>(x), static_cast<cudaStream_t>(stream));
     if (rc != LORDS_OK) return rc;
     st.last_launches = 1;
     st.last_path = "checkpoint_load";

@@ -1,7 +1,7 @@
 // y = x W^T on microscaled 4-bit operands, for many tokens: tcgen05.mma kind::mxf4 on CTA pairs (cta_group::2).
 //
 // A pair computes 256 tokens x BN out-features; the tokens are the MMA's rows, so that a thread of the epilogue holds one token's
-// neighbouring out-features and stores whole sectors.  A step is 256 columns, 128 bytes of codes a row: each CTA loads its 128
+// neighbouring out-features: it puts 128 bytes of them into its row of a shared-memory tile, which leaves by TMA.  A step is 256 columns, 128 bytes of codes a row: each CTA loads its 128
 // tokens and its half of the out-features by TMA, its tokens' scales and the scales of all BN out-features, which go on to TMEM
 // (tcgen05.cp) ahead of the step's four MMAs.  Tiles are dealt out to as many pairs as are resident; with BN = 128 two accumulators take turns, so
 // that a tile's stores run beside the next one's MMAs, with 256 the loads of the next tile do.
@@ -35,8 +35,9 @@ template <int BN> struct PCfg {
     static constexpr int XSF = 2 * kTileBytes;                   // scales of a step: two tiles of four blocks
     static constexpr int WSF = BN / kTileRows * 2 * kTileBytes;
     static constexpr int STAGE = XTILE + WTILE + XSF + WSF;
-    static constexpr int STAGES = (226 * 1024) / STAGE;
-    static constexpr int SMEM = 1024 + STAGES * STAGE + 256;
+    static constexpr int OUT = EPI * 4096;                       // 32 tokens x 128 bytes of y a warp, on their way out
+    static constexpr int STAGES = (232448 - 1024 - 256 - OUT) / STAGE;
+    static constexpr int SMEM = 1024 + STAGES * STAGE + OUT + 256;
     static constexpr int ACCS = BN <= 128 ? 2 : 1;
     static constexpr uint32_t SF_COL = ACCS * BN;                // behind the accumulators: two sets of scales of a step
     static constexpr uint32_t SF_COLS = 8 + BN / kTileRows * 8;
@@ -48,6 +49,8 @@ struct alignas(64) PairParams {
     CUtensorMap tm_w;        // bytes [m][pitch], box {128, BN / 2}
     CUtensorMap tm_xs;       // scale tiles as words [row tiles][128 ktiles], box {256, 1}
     CUtensorMap tm_ws;       // the same, box {256, BN / 128}
+    CUtensorMap tm_y;        // y, box {128 bytes, 32 rows}, 128-byte swizzle; used if rows of y are 16-byte multiples
+    int y_by_tma;
     int M, m;
     int tok_tiles, tiles, steps, blocks;
     int pairs;
@@ -61,12 +64,15 @@ __device__ __forceinline__ uint32_t pack_bf16(uint32_t lo, uint32_t hi)
     const __nv_bfloat162 v = __floats2bfloat162_rn(__uint_as_float(lo), __uint_as_float(hi));
     return *reinterpret_cast<const uint32_t *>(&v);
 }
-__device__ __forceinline__ void store_sector(void *at, const uint32_t *w)
+// A tile of shared memory to global memory, rows and columns outside the tensor left out; a group of its own.
+__device__ __forceinline__ void tma_store_2d(const void *tmap, int x, int y, uint32_t src)
 {
-    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]),
-                 "r"(w[7])
-                 : "memory");
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];" ::"l"(tmap), "r"(src), "r"(x), "r"(y) : "memory");
+    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
 }
+// The thread's stores have read their shared memory / have been done.
+__device__ __forceinline__ void tma_store_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
+__device__ __forceinline__ void tma_store_wait() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 
 template <int BN>
 __global__ void __launch_bounds__(PCfg<BN>::THREADS, 1) lords_mxfp4_pair_kernel(const __grid_constant__ PairParams p)
@@ -75,7 +81,7 @@ __global__ void __launch_bounds__(PCfg<BN>::THREADS, 1) lords_mxfp4_pair_kernel(
     constexpr int STAGES = C::STAGES;
     extern __shared__ uint8_t p_smem[];
     const uint32_t base = (smem_u32(p_smem) + 1023u) & ~1023u;
-    const uint32_t bars = base + STAGES * C::STAGE;
+    const uint32_t out_s = base + STAGES * C::STAGE, bars = out_s + C::OUT;
     const uint32_t bar_full = bars, bar_empty = bars + 8 * STAGES, bar_acc_full = bar_empty + 8 * STAGES, bar_acc_empty = bar_acc_full + 16;
     const uint32_t tmem_slot = bar_acc_empty + 16;
     static_assert(8 * (2 * STAGES + 4) + 4 <= 256, "barrier area");
@@ -166,51 +172,79 @@ __global__ void __launch_bounds__(PCfg<BN>::THREADS, 1) lords_mxfp4_pair_kernel(
         constexpr int CW = BN / (C::EPI / 4);
         const uint32_t empty0 = map_to_rank(bar_acc_empty, 0);
         const uint32_t acc = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(ch * CW);
-        const size_t row_bytes = (size_t)p.m * (p.y_f32 ? 4 : 2);
+        const uint32_t own = out_s + (uint32_t)((warp - kPEpiWarp0) * 4096), row = own + (uint32_t)(lane * 128);
         int n = 0;
         for (int tile = pair; tile < p.tiles; tile += p.pairs, ++n) {
             const int a = n % C::ACCS, wt = tile / p.tok_tiles, tt = tile - wt * p.tok_tiles;
             if (!__all_sync(0xffffffffu, mbar_wait_cluster(bar_acc_full + 8 * a, (uint32_t)((n / C::ACCS) & 1), status, 75))) { failed = true; break; }
             tc_fence_after_sync();
-            const int t = tt * kPTokens + rank * 128 + q * 32 + lane;
-#pragma unroll 1
-            for (int c0 = 0; c0 < CW; c0 += 32) {
-                uint32_t v[32];
+            const int t0 = tt * kPTokens + rank * 128 + q * 32, t = t0 + lane;
+            auto put = [&](int c, const uint32_t *w) {        // 16 bytes of the thread's row, chunk c of 8
+                sts_v4(row + (uint32_t)((c ^ (lane & 7)) << 4), make_uint4(w[0], w[1], w[2], w[3]));
+            };
+            auto leave = [&](int i) {                          // 128 bytes of 32 tokens, from out-feature i on
+                fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0 && t0 < p.M && i < p.m) tma_store_2d(&p.tm_y, i, t0, own);
+            };
+            auto load = [&](int c0, uint32_t (&v)[32]) {
                 tmem_ld_32x32(acc + (uint32_t)(a * BN + c0), v);
                 tmem_wait_ld(v);
-                if (c0 + 32 == CW) {            // the accumulator has been read
-                    tc_fence_before_sync();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive_pair(empty0 + 8 * a);
+            };
+            auto release = [&]() {                             // the accumulator has been read
+                tc_fence_before_sync();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_pair(empty0 + 8 * a);
+            };
+            auto room = [&]() {                                // what left last has been read from the warp's tile
+                if (lane == 0) tma_store_wait_read();
+                __syncwarp();
+            };
+            const int i0 = wt * BN + ch * CW;
+            if (!p.y_by_tma) {
+#pragma unroll 1
+                for (int c0 = 0; c0 < CW; c0 += 32) {
+                    uint32_t v[32];
+                    load(c0, v);
+                    if (c0 + 32 == CW) release();
+                    if (t < p.M)
+#pragma unroll
+                        for (int c = 0; c < 32; ++c)
+                            if (i0 + c0 + c < p.m) store_out(p.y, p.y_f32, (size_t)t * p.m + i0 + c0 + c, __uint_as_float(v[c]));
                 }
-                const int i = wt * BN + ch * CW + c0;
-                if (t >= p.M || i >= p.m) continue;
-                if (p.y_f32) {
-                    float *dst = static_cast<float *>(p.y) + (size_t)t * p.m + i;
-                    if (i + 32 <= p.m && (row_bytes & 31) == 0 && (reinterpret_cast<uintptr_t>(p.y) & 31) == 0) {
+            } else if (p.y_f32) {
+#pragma unroll 1
+                for (int c0 = 0; c0 < CW; c0 += 32) {
+                    uint32_t v[32];
+                    load(c0, v);
+                    if (c0 + 32 == CW) release();
+                    room();
 #pragma unroll
-                        for (int g = 0; g < 4; ++g) store_sector(dst + 8 * g, v + 8 * g);
-                    } else {
+                    for (int c = 0; c < 8; ++c) put(c, v + 4 * c);
+                    leave(i0 + c0);
+                }
+            } else {
+                // all of it into registers first, so that the next tile's MMAs wait no longer than that takes
+                uint32_t w[CW / 2];
 #pragma unroll
-                        for (int c = 0; c < 32; ++c)
-                            if (i + c < p.m) dst[c] = __uint_as_float(v[c]);
-                    }
-                } else {
-                    uint32_t w[16];
+                for (int c0 = 0; c0 < CW; c0 += 32) {
+                    uint32_t v[32];
+                    load(c0, v);
 #pragma unroll
-                    for (int c = 0; c < 16; ++c) w[c] = pack_bf16(v[2 * c], v[2 * c + 1]);
-                    uint16_t *dst = static_cast<uint16_t *>(p.y) + (size_t)t * p.m + i;
-                    if (i + 32 <= p.m && (row_bytes & 31) == 0 && (reinterpret_cast<uintptr_t>(p.y) & 31) == 0) {
-                        store_sector(dst, w);
-                        store_sector(dst + 16, w + 8);
-                    } else {
+                    for (int c = 0; c < 16; ++c) w[c0 / 2 + c] = pack_bf16(v[2 * c], v[2 * c + 1]);
+                }
+                release();
 #pragma unroll
-                        for (int c = 0; c < 32; ++c)
-                            if (i + c < p.m) dst[c] = (uint16_t)(w[c >> 1] >> (16 * (c & 1)));
-                    }
+                for (int c0 = 0; c0 < CW; c0 += 64) {
+                    room();
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) put(c, w + c0 / 2 + 4 * c);
+                    leave(i0 + c0);
                 }
             }
         }
+        if (lane == 0) tma_store_wait();
+        __syncwarp();
     }
 
     if (failed) ptx::record_give_up(p.status, LORDS_ERR_TIMEOUT);
@@ -272,6 +306,11 @@ template <int BN> int run_pair(const MxProblem &p, State &st, cudaStream_t strea
         !make_map_2d(&k.tm_xs, CU_TENSOR_MAP_DATA_TYPE_INT32, 4, p.xs, words, xt, 256, 1, CU_TENSOR_MAP_SWIZZLE_NONE) ||
         !make_map_2d(&k.tm_ws, CU_TENSOR_MAP_DATA_TYPE_INT32, 4, p.ws, words, wt, 256, BN / kTileRows, CU_TENSOR_MAP_SWIZZLE_NONE))
         return LORDS_ERR_CUDA;
+    k.y_by_tma = ((size_t)p.m * (p.y_f32 ? 4 : 2)) % 16 == 0;
+    k.tm_y = k.tm_x;
+    if (k.y_by_tma && !make_map_2d(&k.tm_y, p.y_f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, p.y_f32 ? 4 : 2, p.y, (uint64_t)p.m,
+                                   (uint64_t)p.M, p.y_f32 ? 32 : 64, 32, CU_TENSOR_MAP_SWIZZLE_128B))
+        return LORDS_ERR_CUDA;
     k.M = p.M; k.m = p.m;
     k.tok_tiles = (p.M + kPTokens - 1) / kPTokens;
     const long long tiles = (long long)k.tok_tiles * ((p.m + BN - 1) / BN);
@@ -296,10 +335,10 @@ template <int BN> int run_pair(const MxProblem &p, State &st, cudaStream_t strea
 int launch_mxfp4_pair(const MxProblem &p, State &st, cudaStream_t stream)
 {
     if (p.x) return LORDS_ERR_UNSUPPORTED;
-    const long long tok = (p.M + kPTokens - 1) / kPTokens;
-    // 256 out-features a pair where they fill the pairs' waves as well as 128 do
-    const long long w256 = (tok * ((p.m + 255) / 256) + 73) / 74, w128 = (tok * ((p.m + 127) / 128) + 73) / 74;
-    return 2 * w256 <= w128 ? run_pair<256>(p, st, stream) : run_pair<128>(p, st, stream);
+    // Microseconds of a launch: waves of tiles, a step's and a tile's fixed part measured at 2048 tokens.
+    const double steps = (p.n + 255) / 256;
+    const long long tok = (p.M + kPTokens - 1) / kPTokens, w256 = (tok * ((p.m + 255) / 256) + 73) / 74, w128 = (tok * ((p.m + 127) / 128) + 73) / 74;
+    return (double)w256 * (0.37 * steps + 1.8) <= (double)w128 * (0.31 * steps + 0.6) ? run_pair<256>(p, st, stream) : run_pair<128>(p, st, stream);
 }
 
 }  // namespace lords
