@@ -41,10 +41,6 @@ def _load():
         "lords_strerror": (cs, [ci]),
         "lords_equivalent_rank": (i64, [i64, i64, i64]),
         "lords_packed_bytes": (i64, [i64, i64, ci]),
-        "lords_mxfp4_codes_bytes": (i64, [i64, i64]),
-        "lords_mxfp4_scales_bytes": (i64, [i64, i64]),
-        "lords_checkpoint_bytes": (i64, [i64, i64]),
-        "lords_checkpoint_scales_bytes": (i64, [i64, i64]),
         "lords_pack_codes": (ci, [p, i64, i64, ci, p]),
         "lords_unpack_codes": (ci, [p, i64, i64, ci, p]),
         "lords_init": (ci, [ci, sz]),
@@ -109,29 +105,6 @@ def lords_packed_bytes(m: int, n: int, bits: int) -> int:
     return v
 
 
-def _bytes_of(name: str, rows: int, cols: int) -> int:
-    v = int(getattr(_load(), name)(rows, cols))
-    if v < 0:
-        raise LordsError(v, name)
-    return v
-
-
-def lords_mxfp4_codes_bytes(rows: int, cols: int) -> int:
-    return _bytes_of("lords_mxfp4_codes_bytes", rows, cols)
-
-
-def lords_mxfp4_scales_bytes(rows: int, cols: int) -> int:
-    return _bytes_of("lords_mxfp4_scales_bytes", rows, cols)
-
-
-def lords_checkpoint_bytes(M: int, n: int) -> int:
-    return _bytes_of("lords_checkpoint_bytes", M, n)
-
-
-def lords_checkpoint_scales_bytes(M: int, n: int) -> int:
-    return _bytes_of("lords_checkpoint_scales_bytes", M, n)
-
-
 def lords_pack_codes(codes: np.ndarray, bits: int) -> np.ndarray:
     """Host: uint8 codes [m, n] -> packed uint8 [m, n*bits/8]."""
     codes = np.ascontiguousarray(codes, dtype=np.uint8)
@@ -173,13 +146,14 @@ def _cb_ptr(codebook, bits):
     return cb
 
 
-# The calls that take tensors are native functions (csrc/lords_module.cc): a small layer runs in a few
+# The calls that take tensors (and the sizes that go with them) are native functions (csrc/lords_module.cc): a small layer runs in a few
 # microseconds, which is less than marshalling a dozen arguments in Python takes.
 _TENSOR_CALLS = ("lords_linear_forward", "lords_linear_forward_bits", "lords_linear_forward_f32", "lords_linear_forward_host",
                  "lords_linear_forward_noalloc", "lords_quantize_codes", "lords_transpose_codes", "lords_linear_backward_input",
                  "lords_linear_backward_input_f32", "lords_linear_backward_factors", "lords_linear_backward_qat",
-                 "lords_blockscale_forward", "lords_adapter_forward", "lords_mxfp4_quantize", "lords_mxfp4_dequantize", "lords_mxfp4_matmul",
-                 "lords_mxfp4_forward", "lords_checkpoint_store", "lords_checkpoint_load", "lords_linear_backward_factors_checkpoint",
+                 "lords_blockscale_forward", "lords_adapter_forward", "lords_mxfp4_codes_bytes", "lords_mxfp4_scales_bytes",
+                 "lords_mxfp4_quantize", "lords_mxfp4_dequantize", "lords_mxfp4_matmul", "lords_mxfp4_forward", "lords_checkpoint_bytes",
+                 "lords_checkpoint_scales_bytes", "lords_checkpoint_store", "lords_checkpoint_load", "lords_linear_backward_factors_checkpoint",
                  "lords_linear_backward_qat_checkpoint")
 
 

@@ -15,41 +15,43 @@ using namespace mx;
 
 constexpr int kCThreads = 256;
 
-// rows of whole blocks and scales of four blocks: what a row of n values takes
-__device__ __forceinline__ int q_pitch(int n) { return blocks_of(n) * kBlock; }
-__device__ __forceinline__ int e_pitch(int n) { return scale_tiles_of(n) * kTileBlocks; }
-
-// A CTA takes kCRows rows x 256 columns, a warp four rows, a thread eight values of each.
-constexpr int kCPer = 4, kCRows = kCThreads / 32 * kCPer;
-
-__global__ void __launch_bounds__(kCThreads) lords_checkpoint_store_kernel(const uint16_t *__restrict__ x, int M, int n, uint8_t *__restrict__ q,
+// A CTA takes eight warps' rows x 256 columns: a warp PER rows, a thread eight values of each.  Small calls take one row a warp and more CTAs.
+template <int PER>
+__global__ void __launch_bounds__(kCThreads) lords_checkpoint_store_kernel(const uint16_t *__restrict__ x, int M, int n, int qp, int ep, uint8_t *__restrict__ q,
                                                                            uint8_t *__restrict__ e)
 {
-    const int lane = threadIdx.x & 31, t0 = (int)blockIdx.y * kCRows + (threadIdx.x >> 5) * kCPer;
-    const int c = (int)blockIdx.x * 256 + lane * 8, qp = q_pitch(n), ep = e_pitch(n);
+    const int lane = threadIdx.x & 31, t0 = ((int)blockIdx.y * (kCThreads / 32) + (threadIdx.x >> 5)) * PER;
+    const int c = (int)blockIdx.x * 256 + lane * 8;
     const uint16_t *end = x + (size_t)M * n;
-    uint32_t w[kCPer][4];
+    ptx::griddep_launch_dependents();
+    ptx::griddep_wait();
+    uint32_t w[PER][4];
 #pragma unroll
-    for (int k = 0; k < kCPer; ++k) {
+    for (int k = 0; k < PER; ++k) {
         w[k][0] = w[k][1] = w[k][2] = w[k][3] = 0u;
         if (t0 + k < M && c < n) load8(x + (size_t)(t0 + k) * n, n, c, end, w[k]);
     }
 #pragma unroll
-    for (int k = 0; k < kCPer; ++k) {
-        uint32_t top = max_magnitudes(max_magnitudes(w[k][0], w[k][1]), max_magnitudes(w[k][2], w[k][3]));
-        top = max_magnitudes(top, __shfl_xor_sync(0xffffffffu, top, 1));
-        top = max_magnitudes(top, __shfl_xor_sync(0xffffffffu, top, 2));
-        const uint32_t byte = scale_byte<0>(max(top & 0xFFFFu, top >> 16));
+    for (int k = 0; k < PER; ++k) {
+        uint32_t top = larger(larger(magnitudes(w[k][0]), magnitudes(w[k][1]), magnitudes(w[k][2])), magnitudes(w[k][3]));
+        top = larger(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = larger(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        const uint32_t byte = scale_byte<0>(larger_half(top));
         if (t0 + k >= M) continue;
-        // whole numbers, value * 2^-E * 64: a bf16 product and a power of two, both exact, so only the conversion rounds
+        // value * 2^-E is exact in bf16; limited to 127/64 (which takes no more than half a step: the largest bf16 number below 2 is 127.5/64), then
+        // times 64 onto 1.5 * 2^23, whose low bits are then the whole number: one rounding, ties to even
         const uint32_t inv = inverse_scale(byte);
-        uint32_t out[2] = {0u, 0u};
+        uint32_t out[2];
 #pragma unroll
-        for (int h = 0; h < 8; ++h) {
-            const uint32_t u = bf16x2_mul(w[k][h >> 1], inv);
-            int i = __float2int_rn(__uint_as_float(h & 1 ? u & 0xFFFF0000u : u << 16) * 64.0f);
-            i = i > 127 ? 127 : i < -127 ? -127 : i;
-            out[h >> 2] |= (uint32_t)(i & 255) << (8 * (h & 3));
+        for (int h = 0; h < 2; ++h) {
+            uint32_t u[2];
+#pragma unroll
+            for (int g = 0; g < 2; ++g) {
+                u[g] = bf16x2_mul(w[k][2 * h + g], inv);
+                asm("min.bf16x2 %0, %0, %1;\nmax.bf16x2 %0, %0, %2;" : "+r"(u[g]) : "r"(0x3FFE3FFEu), "r"(0xBFFEBFFEu));
+            }
+            auto whole = [](float v) { return __float_as_uint(fmaf(v, 64.0f, 12582912.0f)); };
+            out[h] = __byte_perm(__byte_perm(whole(low_half(u[0])), whole(high_half(u[0])), 0x0040), __byte_perm(whole(low_half(u[1])), whole(high_half(u[1])), 0x0040), 0x5410);
         }
         if (byte == 255u) out[0] = out[1] = 0u;
         if (c < qp) *reinterpret_cast<uint2 *>(q + (size_t)(t0 + k) * qp + c) = make_uint2(out[0], out[1]);
@@ -73,42 +75,46 @@ __device__ __forceinline__ uint4 values8(uint2 q, uint32_t byte)
     return make_uint4(v[0], v[1], v[2], v[3]);
 }
 
-__global__ void __launch_bounds__(kCThreads) lords_checkpoint_load_kernel(const uint8_t *__restrict__ q, const uint8_t *__restrict__ e, int M, int n,
+template <int PER>
+__global__ void __launch_bounds__(kCThreads) lords_checkpoint_load_kernel(const uint8_t *__restrict__ q, const uint8_t *__restrict__ e, int M, int n, int qp, int ep,
                                                                           uint16_t *__restrict__ x)
 {
-    const int lane = threadIdx.x & 31, t0 = (int)blockIdx.y * kCRows + (threadIdx.x >> 5) * kCPer;
-    const int c = (int)blockIdx.x * 256 + lane * 8, qp = q_pitch(n), ep = e_pitch(n);
+    const int lane = threadIdx.x & 31, t0 = ((int)blockIdx.y * (kCThreads / 32) + (threadIdx.x >> 5)) * PER;
+    const int c = (int)blockIdx.x * 256 + lane * 8;
+    ptx::griddep_launch_dependents();
+    ptx::griddep_wait();
     if (c >= n) return;
-    uint2 w[kCPer];
-    uint32_t byte[kCPer];
+    uint2 w[PER];
+    uint32_t byte[PER];
 #pragma unroll
-    for (int k = 0; k < kCPer; ++k) {
+    for (int k = 0; k < PER; ++k) {
         const int t = t0 + k < M ? t0 + k : M - 1;
         w[k] = __ldg(reinterpret_cast<const uint2 *>(q + (size_t)t * qp + c));
         byte[k] = __ldg(e + (size_t)t * ep + c / kBlock);
     }
 #pragma unroll
-    for (int k = 0; k < kCPer; ++k)
+    for (int k = 0; k < PER; ++k)
         if (t0 + k < M) store8(x + (size_t)(t0 + k) * n, n, c, values8(w[k], byte[k]));
 }
+
+// One row a warp where four would leave fewer than two CTAs an SM.
+bool small(int M, int n) { return (long long)((M + 31) / 32) * ((n + 255) / 256) < 296; }
+dim3 grid_of(int M, int cols, int per) { return dim3((unsigned)((cols + 255) / 256), (unsigned)((M + 8 * per - 1) / (8 * per))); }
 
 }  // namespace
 
 int launch_checkpoint_store(const uint16_t *x, int M, int n, uint8_t *q, uint8_t *e, cudaStream_t stream)
 {
-    // (whole words of scales are written)
-    const dim3 grid((unsigned)((scale_tiles_of(n) * kTileBlocks * kBlock + 255) / 256), (unsigned)((M + kCRows - 1) / kCRows));
-    lords_checkpoint_store_kernel<<<grid, kCThreads, 0, stream>>>(x, M, n, q, e);
-    LORDS_CUDA_TRY(cudaGetLastError());
-    return LORDS_OK;
+    const int qp = blocks_of(n) * kBlock, ep = scale_tiles_of(n) * kTileBlocks;       // (whole words of scales are written)
+    if (small(M, n)) return launch_dependent(lords_checkpoint_store_kernel<1>, grid_of(M, ep * kBlock, 1), kCThreads, stream, x, M, n, qp, ep, q, e);
+    return launch_dependent(lords_checkpoint_store_kernel<4>, grid_of(M, ep * kBlock, 4), kCThreads, stream, x, M, n, qp, ep, q, e);
 }
 
 int launch_checkpoint_load(const uint8_t *q, const uint8_t *e, int M, int n, uint16_t *x, cudaStream_t stream)
 {
-    const dim3 grid((unsigned)((n + 255) / 256), (unsigned)((M + kCRows - 1) / kCRows));
-    lords_checkpoint_load_kernel<<<grid, kCThreads, 0, stream>>>(q, e, M, n, x);
-    LORDS_CUDA_TRY(cudaGetLastError());
-    return LORDS_OK;
+    const int qp = blocks_of(n) * kBlock, ep = scale_tiles_of(n) * kTileBlocks;
+    if (small(M, n)) return launch_dependent(lords_checkpoint_load_kernel<1>, grid_of(M, n, 1), kCThreads, stream, q, e, M, n, qp, ep, x);
+    return launch_dependent(lords_checkpoint_load_kernel<4>, grid_of(M, n, 4), kCThreads, stream, q, e, M, n, qp, ep, x);
 }
 
 }  // namespace lords

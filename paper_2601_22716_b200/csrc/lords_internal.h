@@ -158,9 +158,24 @@ struct MxProblem {
     void *y;                 // bf16 [M][m] or float [M][m]
     int y_f32;
 };
+// The launches of the format kernels: programmatic dependent launches on both sides; everything is read and written after the previous one's end.
+template <class Kernel, class... Args> inline int launch_dependent(Kernel kernel, dim3 grid, unsigned threads, cudaStream_t stream, Args... args)
+{
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = cudaLaunchConfig_t{};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.stream = stream;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    LORDS_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, args...));
+    return LORDS_OK;
+}
 int launch_mxfp4_quantize(const uint16_t *v, int rows, int cols, uint8_t *codes, uint8_t *scales, uint8_t *codes_t, uint8_t *scales_t, cudaStream_t stream);
 int launch_mxfp4_dequantize(const uint8_t *codes, const uint8_t *scales, int rows, int cols, uint16_t *v, cudaStream_t stream);
-// Few tokens: a CTA per 128 rows of W, the steps divided among a cluster.  x in bf16 (up to 16 tokens; else LORDS_ERR_UNSUPPORTED) or in 4 bits.
+// Few tokens: a CTA per 128 rows of W, the steps divided among a cluster.  x in bf16 (up to four tokens; else LORDS_ERR_UNSUPPORTED) or in 4 bits.
 int launch_mxfp4_stream(const MxProblem &p, State &st, cudaStream_t stream);
 // Many tokens: CTA pairs, 256 tokens x 128 or 256 out-features.  x in 4 bits.
 int launch_mxfp4_pair(const MxProblem &p, State &st, cudaStream_t stream);

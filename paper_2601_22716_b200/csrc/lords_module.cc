@@ -335,6 +335,27 @@ PyObject *py_lords_adapter_forward(PyObject *, PyObject *const *args, Py_ssize_t
     return done(status, "lords_adapter_forward");
 }
 
+// Sizes of a microscaled tensor's parts: rows and columns in, bytes out.
+PyObject *size_call(const char *fn, int64_t (*call)(int64_t, int64_t), PyObject **a)
+{
+    const long long r = PyLong_AsLongLong(a[0]);
+    if (r == -1 && PyErr_Occurred()) return nullptr;
+    const long long c = PyLong_AsLongLong(a[1]);
+    if (c == -1 && PyErr_Occurred()) return nullptr;
+    const int64_t v = call(r, c);
+    return v < 0 ? done((int)v, fn) : PyLong_FromLongLong(v);
+}
+#define LORDS_SIZE(NAME, R, C)                                                                              \
+    PyObject *py_##NAME(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyObject *kwnames)             \
+    {                                                                                                       \
+        LORDS_ARGS(#NAME, 2, 2, R, C);                                                                      \
+        return size_call(#NAME, NAME, a);                                                                   \
+    }
+LORDS_SIZE(lords_mxfp4_codes_bytes, "rows", "cols")
+LORDS_SIZE(lords_mxfp4_scales_bytes, "rows", "cols")
+LORDS_SIZE(lords_checkpoint_bytes, "M", "n")
+LORDS_SIZE(lords_checkpoint_scales_bytes, "M", "n")
+
 PyObject *py_lords_mxfp4_quantize(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyObject *kwnames)
 {
     LORDS_ARGS("lords_mxfp4_quantize", 8, 5, "v", "rows", "cols", "codes", "scales", "codes_t", "scales_t", "stream");
@@ -493,6 +514,10 @@ PyMethodDef g_methods[] = {
               "Comparator (Eq. 2): y = x (L[Q] (.) (s (x) 1))^T; y is bf16 [M, m], or float with f32=True."),
     LORDS_DEF(lords_adapter_forward, "lords_adapter_forward(x, Qpacked, scales, A_l, B_l, codebook, bits, blk, M, m, n, r, y, stream=None, f32=False)\n--\n\n"
               "Comparator (Sec. 3.4 / 4.4): the block-scaled layer plus an additive rank-r adapter, three launches."),
+    LORDS_DEF(lords_mxfp4_codes_bytes, "lords_mxfp4_codes_bytes(rows, cols)\n--\n\nBytes of the codes of a 4-bit tensor of rows x cols."),
+    LORDS_DEF(lords_mxfp4_scales_bytes, "lords_mxfp4_scales_bytes(rows, cols)\n--\n\nBytes of its scales."),
+    LORDS_DEF(lords_checkpoint_bytes, "lords_checkpoint_bytes(M, n)\n--\n\nBytes of the values of an 8-bit checkpoint of M x n."),
+    LORDS_DEF(lords_checkpoint_scales_bytes, "lords_checkpoint_scales_bytes(M, n)\n--\n\nBytes of its scales."),
     LORDS_DEF(lords_mxfp4_quantize, "lords_mxfp4_quantize(v, rows, cols, codes, scales, codes_t=None, scales_t=None, stream=None)\n--\n\n"
               "bf16 [rows, cols] to 4 bits in blocks along the rows (codes, scales) and / or along the columns (codes_t, scales_t); either pair may be None."),
     LORDS_DEF(lords_mxfp4_dequantize, "lords_mxfp4_dequantize(codes, scales, rows, cols, v, stream=None)\n--\n\n"

@@ -28,13 +28,12 @@ __host__ __device__ inline size_t codes_pitch(int cols) { return (size_t)blocks_
 // Where the scale of row i and block b of a tile lies inside it: four words a lane, a word the four blocks of row 32 j + lane.
 __host__ __device__ inline int scale_at(int i, int b) { return (i & 31) * 16 + (i >> 5) * 4 + b; }
 
-// The larger magnitudes of two pairs of bf16 values; a NaN in either stays one.
-__device__ __forceinline__ uint32_t max_magnitudes(uint32_t a, uint32_t b)
-{
-    uint32_t d;
-    asm("{\n.reg .b32 u, v;\nabs.bf16x2 u, %1;\nabs.bf16x2 v, %2;\nmax.NaN.bf16x2 %0, u, v;\n}\n" : "=r"(d) : "r"(a), "r"(b));
-    return d;
-}
+// Magnitudes of a pair of bf16 values, and the larger ones of two or three pairs of magnitudes: as whole numbers they are in order, infinities and NaNs
+// above all others.
+__device__ __forceinline__ uint32_t magnitudes(uint32_t w) { return w & 0x7FFF7FFFu; }
+__device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) { return __vmaxu2(a, b); }
+__device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b, uint32_t c) { return __vimax3_u16x2(a, b, c); }
+__device__ __forceinline__ uint32_t larger_half(uint32_t top) { return max(top & 0xFFFFu, top >> 16); }
 __device__ __forceinline__ uint32_t bf16x2_mul(uint32_t a, uint32_t b)
 {
     uint32_t d;
@@ -43,7 +42,7 @@ __device__ __forceinline__ uint32_t bf16x2_mul(uint32_t a, uint32_t b)
 }
 
 // Eight values of a row of `cols` from column c (below cols) on, as pairs, zeros behind the last.  `end`: behind the matrix.
-__device__ __forceinline__ void load8(const uint16_t *__restrict__ row, int cols, int c, const uint16_t *end, uint32_t (&w)[4])
+__device__ __forceinline__ void load8(const uint16_t *__restrict__ row, int cols, int c, const uint16_t *end, uint32_t *w)
 {
     const uint16_t *src = row + c;
     if ((cols & 7) == 0) {
@@ -85,19 +84,10 @@ __device__ __forceinline__ uint32_t inverse_scale(uint32_t byte)
     return s | s << 16;
 }
 
-// Eight bf16 values (pairs, low half first) to eight 4-bit codes, low nibble first.  The product with 2^-E is exact: what falls out of bf16's range
-// below is far from the least code.  (Infinities and NaNs times the zero that stands for 2^-E of such a block are NaN, which the
-// conversion makes 6: zeroed at the end.)
-__device__ __forceinline__ uint32_t to_codes4(const uint32_t (&w)[4], uint32_t byte)
+// Eight bf16 values, times 2^-E already, to eight 4-bit codes, low nibble first: the first of each pair `a`, the second of each pair `b`.  (The
+// product with 2^-E is exact: what falls out of bf16's range below is far from the least code.)
+__device__ __forceinline__ uint32_t codes_of(float a0, float b0, float a1, float b1, float a2, float b2, float a3, float b3)
 {
-    const uint32_t inv = inverse_scale(byte);
-    float v[8];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        const uint32_t u = bf16x2_mul(w[k], inv);
-        v[2 * k] = __uint_as_float(u << 16);
-        v[2 * k + 1] = __uint_as_float(u & 0xFFFF0000u);
-    }
     uint32_t c;
     asm("{\n"
         ".reg .b8 b0, b1, b2, b3;\n"
@@ -108,7 +98,18 @@ __device__ __forceinline__ uint32_t to_codes4(const uint32_t (&w)[4], uint32_t b
         "mov.b32 %0, {b0, b1, b2, b3};\n"
         "}\n"
         : "=r"(c)
-        : "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]));
+        : "f"(a0), "f"(b0), "f"(a1), "f"(b1), "f"(a2), "f"(b2), "f"(a3), "f"(b3));
+    return c;
+}
+__device__ __forceinline__ float low_half(uint32_t u) { return __uint_as_float(u << 16); }
+__device__ __forceinline__ float high_half(uint32_t u) { return __uint_as_float(u & 0xFFFF0000u); }
+// Eight bf16 values as pairs, low half first, with the block's scale byte.  (Infinities and NaNs times the zero that stands for 2^-E of a block that is
+// not finite are NaN, which the conversion makes 6: zeroed at the end.)
+__device__ __forceinline__ uint32_t to_codes4(const uint32_t *w, uint32_t byte)
+{
+    const uint32_t inv = inverse_scale(byte);
+    const uint32_t u0 = bf16x2_mul(w[0], inv), u1 = bf16x2_mul(w[1], inv), u2 = bf16x2_mul(w[2], inv), u3 = bf16x2_mul(w[3], inv);
+    const uint32_t c = codes_of(low_half(u0), high_half(u0), low_half(u1), high_half(u1), low_half(u2), high_half(u2), low_half(u3), high_half(u3));
     return byte == 255u ? 0u : c;
 }
 
@@ -116,11 +117,10 @@ __device__ __forceinline__ uint32_t to_codes4(const uint32_t (&w)[4], uint32_t b
 
 namespace ptx {
 
-// A copy of whole 16-byte words from global into this CTA's shared memory, its bytes counted on `bar`.
-__device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar)
+// Whole 16-byte words from global into this CTA's shared memory, counted in bytes on `bar`.
+__device__ __forceinline__ void load_words(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar)
 {
-    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar)
-                 : "memory");
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
 // A tile of scales (512 bytes, 32 rows of 16) into four TMEM columns, the 32 lanes repeated in all four quadrants; ordered before the MMAs that
 // the same thread issues next, and after those it has issued.

@@ -14,90 +14,136 @@ namespace {
 using namespace mx;
 
 // ------------------------------------------------------------------------------------------------ to 4 bits
-// A CTA takes ROWS rows x 128 columns.  Along the rows, four neighbouring threads hold a block in registers.  Along the columns, a thread reads
-// two columns x 32 rows back from shared memory.  Scales meet in shared memory as words of four blocks.
-#ifndef QROWS
-#define QROWS 64
-#endif
+// A CTA takes 64 rows x 128 columns.  Along the rows, two neighbouring threads hold a block in registers, sixteen values each.  Along the columns, a
+// thread reads two columns x 32 rows back from shared memory.  Scales meet in shared memory as words of four blocks.
+//
+// 14336 x 4096: rows 23.3 us (6.4 TB/s, the copy rate; 30.7 with four threads to a block and 12.6 instructions a value, which kept the issue slots 81 %
+// busy), columns 30.6, both 36 (46.5 with 16-byte stores along the columns; 5.0 TB/s: issue slots 63 % busy, the load/store unit with
+// the tile's way through shared memory).
+constexpr int kQRows = 64;                  // rows per CTA (128: 4 to 8 % slower along the rows and level otherwise; 32: 2 to 10 % slower)
 constexpr int kQThreads = 256;
 constexpr int kQPitch = 128 * 2 + 16;       // bytes per row of the tile in shared memory; 16-byte words stay aligned
+constexpr int kQBlock = 32 * kQPitch + 64;  // ... and per 32 rows: the same columns of two neighbouring blocks lie in different banks
 
 struct QuantizeParams {
     const uint16_t *v;       // bf16 [rows][cols]
     uint8_t *codes, *scales;         // blocks along the rows (null: not asked for)
     uint8_t *codes_t, *scales_t;     // blocks along the columns: the same for the transposed matrix (null: not asked for)
     int rows, cols;
+    int pitch, pitch_t;              // bytes of a row of codes
+    int ktiles, ktiles_t;            // tiles of scales in a row of them
+    int wide, wide_t;                // rows of v, and of codes_t, begin at 32-byte boundaries
 };
 
-template <int ROWS, bool ALONG, bool ACROSS> __global__ void __launch_bounds__(kQThreads) lords_mxfp4_quantize_kernel(const QuantizeParams p)
+template <bool ALONG, bool ACROSS> __global__ void __launch_bounds__(kQThreads) lords_mxfp4_quantize_kernel(const QuantizeParams p)
 {
-    constexpr int PER = ROWS / 16;          // rows a thread loads eight values of
-    __shared__ __align__(16) uint8_t tile[ACROSS ? ROWS * kQPitch : 16];
-    __shared__ __align__(16) uint8_t sc[ROWS * 4], sct[kTileBytes];
-    const int tid = threadIdx.x, r0 = (int)blockIdx.y * ROWS, c0 = (int)blockIdx.x * 128;
-    const int seg = tid & 15, row_in = tid >> 4, c = c0 + seg * 8;
-    const uint16_t *end = p.v + (size_t)p.rows * p.cols;
-    uint32_t w[PER][4];
+    constexpr int PER = kQRows / 32;          // rows a thread loads sixteen values of
+    __shared__ __align__(16) uint8_t tile[ACROSS ? kQRows / 32 * kQBlock : 16];
+    __shared__ __align__(16) uint8_t sc[kQRows * 4], sct[128 * (kQRows / 32)];
+    const int tid = threadIdx.x, r0 = (int)blockIdx.y * kQRows, c0 = (int)blockIdx.x * 128;
+    const int seg = tid & 7, row_in = tid >> 3, c = c0 + seg * 16;
+    ptx::griddep_launch_dependents();
+    ptx::griddep_wait();
+    uint32_t w[PER][8];
+    const uint16_t *src = p.v + (size_t)(r0 + row_in) * p.cols + c;
 #pragma unroll
-    for (int k = 0; k < PER; ++k) {
-        const int i = r0 + k * 16 + row_in;
-        w[k][0] = w[k][1] = w[k][2] = w[k][3] = 0u;
-        if (i < p.rows && c < p.cols) load8(p.v + (size_t)i * p.cols, p.cols, c, end, w[k]);
+    for (int k = 0; k < PER; ++k, src += (size_t)32 * p.cols) {
+        const int i = r0 + k * 32 + row_in;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[k][e] = 0u;
+        if (i >= p.rows) continue;
+        if (p.wide) {
+            if (c < p.cols)
+                asm volatile("ld.global.nc.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                             : "=r"(w[k][0]), "=r"(w[k][1]), "=r"(w[k][2]), "=r"(w[k][3]), "=r"(w[k][4]), "=r"(w[k][5]), "=r"(w[k][6]), "=r"(w[k][7])
+                             : "l"(src));
+        } else {
+            const uint16_t *end = p.v + (size_t)p.rows * p.cols;
+            if (c < p.cols) load8(src - c, p.cols, c, end, w[k]);
+            if (c + 8 < p.cols) load8(src - c, p.cols, c + 8, end, w[k] + 4);
+        }
     }
+    uint8_t *out_at = p.codes + (size_t)(r0 + row_in) * p.pitch + c / 2;
 #pragma unroll
     for (int k = 0; k < PER; ++k) {
-        const int rl = k * 16 + row_in;
-        if constexpr (ACROSS) *reinterpret_cast<uint4 *>(tile + rl * kQPitch + seg * 16) = make_uint4(w[k][0], w[k][1], w[k][2], w[k][3]);
+        const int rl = k * 32 + row_in;
+        if constexpr (ACROSS) {
+            uint4 *at = reinterpret_cast<uint4 *>(tile + k * kQBlock + row_in * kQPitch + seg * 32);
+            at[0] = make_uint4(w[k][0], w[k][1], w[k][2], w[k][3]);
+            at[1] = make_uint4(w[k][4], w[k][5], w[k][6], w[k][7]);
+        }
         if constexpr (ALONG) {
-            uint32_t top = max_magnitudes(max_magnitudes(w[k][0], w[k][1]), max_magnitudes(w[k][2], w[k][3]));
-            top = max_magnitudes(top, __shfl_xor_sync(0xffffffffu, top, 1));
-            top = max_magnitudes(top, __shfl_xor_sync(0xffffffffu, top, 2));
-            const uint32_t byte = scale_byte<2>(max(top & 0xFFFFu, top >> 16));
-            if (r0 + rl < p.rows && c < (int)codes_pitch(p.cols) * 2)
-                *reinterpret_cast<uint32_t *>(p.codes + (size_t)(r0 + rl) * codes_pitch(p.cols) + c / 2) = to_codes4(w[k], byte);
-            if ((seg & 3) == 0) sc[rl * 4 + (seg >> 2)] = (uint8_t)byte;
+            uint32_t top = larger(magnitudes(w[k][0]), magnitudes(w[k][1]), magnitudes(w[k][2]));
+            top = larger(top, magnitudes(w[k][3]), magnitudes(w[k][4]));
+            top = larger(top, magnitudes(w[k][5]), magnitudes(w[k][6]));
+            top = larger(top, magnitudes(w[k][7]));
+            top = larger(top, __shfl_xor_sync(0xffffffffu, top, 1));
+            const uint32_t byte = scale_byte<2>(larger_half(top));
+            if (r0 + rl < p.rows && c < p.pitch * 2)
+                *reinterpret_cast<uint2 *>(out_at + (size_t)(k * 32) * p.pitch) = make_uint2(to_codes4(w[k], byte), to_codes4(w[k] + 4, byte));
+            if ((seg & 1) == 0) sc[rl * 4 + (seg >> 1)] = (uint8_t)byte;
         }
     }
     __syncthreads();
     // a row's four scales are a word of the tile of scales; the rows behind the last are part of it
-    if (ALONG && tid < ROWS) {
+    if (ALONG && tid < kQRows) {
         const int i = r0 + tid;
-        *reinterpret_cast<uint32_t *>(p.scales + ((size_t)(i / kTileRows) * scale_tiles_of(p.cols) + blockIdx.x) * kTileBytes + scale_at(i % kTileRows, 0)) =
+        *reinterpret_cast<uint32_t *>(p.scales + ((size_t)(i / kTileRows) * p.ktiles + blockIdx.x) * kTileBytes + scale_at(i % kTileRows, 0)) =
             *reinterpret_cast<const uint32_t *>(sc + tid * 4);
     }
     if constexpr (ACROSS) {
-        for (int e = tid; e < 64 * (ROWS / 32); e += kQThreads) {
-            const int pair = e & 63, b = e >> 6;        // two columns, a block of 32 rows
+        // two columns x 32 rows a thread; the lanes l and l + 16 of a warp have the same columns of neighbouring blocks and exchange halves, so that
+        // each stores 32 bytes, a whole sector, of one column
+        const int lane = tid & 31;
+        for (int e = tid >> 5; e < 4 * (kQRows / 64); e += kQThreads / 32) {
+            const int pair = (e & 3) * 16 + (lane & 15), half = lane >> 4, b = (e >> 2) * 2 + half;
+            const uint8_t *at = tile + b * kQBlock + pair * 4;
             uint32_t u[32];
-            uint32_t top = 0u;
 #pragma unroll
-            for (int k = 0; k < 32; ++k) {
-                u[k] = *reinterpret_cast<const uint32_t *>(tile + (b * 32 + k) * kQPitch + pair * 4);
-                top = max_magnitudes(top, u[k]);
+            for (int k = 0; k < 32; ++k) u[k] = *reinterpret_cast<const uint32_t *>(at + k * kQPitch);
+            uint32_t top = magnitudes(u[0]);
+#pragma unroll
+            for (int k = 1; k < 31; k += 2) top = larger(top, magnitudes(u[k]), magnitudes(u[k + 1]));
+            top = larger(top, magnitudes(u[31]));
+            const uint32_t byte0 = scale_byte<2>(top & 0xFFFFu), byte1 = scale_byte<2>(top >> 16);
+            const uint32_t inv = __byte_perm(inverse_scale(byte0), inverse_scale(byte1), 0x5410);       // each column its own
+#pragma unroll
+            for (int k = 0; k < 32; ++k) u[k] = bf16x2_mul(u[k], inv);
+            uint32_t o0[4], o1[4], out[8];
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const uint32_t *x = u + 8 * g;
+                o0[g] = codes_of(low_half(x[0]), low_half(x[1]), low_half(x[2]), low_half(x[3]), low_half(x[4]), low_half(x[5]), low_half(x[6]), low_half(x[7]));
+                o1[g] = codes_of(high_half(x[0]), high_half(x[1]), high_half(x[2]), high_half(x[3]), high_half(x[4]), high_half(x[5]), high_half(x[6]), high_half(x[7]));
+                if (byte0 == 255u) o0[g] = 0u;
+                if (byte1 == 255u) o1[g] = 0u;
             }
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const uint32_t byte = scale_byte<2>(h ? top >> 16 : top & 0xFFFFu);
-                uint32_t out[4];
-#pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    uint32_t x[4];
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) x[k] = __byte_perm(u[8 * g + 2 * k], u[8 * g + 2 * k + 1], h ? 0x7632 : 0x5410);
-                    out[g] = to_codes4(x, byte);
+            for (int g = 0; g < 4; ++g) {
+                const uint32_t theirs = __shfl_xor_sync(0xffffffffu, half ? o0[g] : o1[g], 16);
+                out[g] = half ? theirs : o0[g];
+                out[4 + g] = half ? o1[g] : theirs;
+            }
+            const int col = c0 + 2 * pair + half, r = r0 + (b & ~1) * 32;
+            if (col < p.cols && r < p.rows) {
+                uint8_t *dst = p.codes_t + (size_t)col * p.pitch_t + r / 2;
+                if (p.wide_t) {
+                    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(dst), "r"(out[0]), "r"(out[1]), "r"(out[2]), "r"(out[3]), "r"(out[4]),
+                                 "r"(out[5]), "r"(out[6]), "r"(out[7])
+                                 : "memory");
+                } else {
+                    *reinterpret_cast<uint4 *>(dst) = make_uint4(out[0], out[1], out[2], out[3]);
+                    if (r + 32 < p.rows) *reinterpret_cast<uint4 *>(dst + 16) = make_uint4(out[4], out[5], out[6], out[7]);
                 }
-                const int col = c0 + 2 * pair + h, r = r0 + b * 32;
-                if (col < p.cols && r < p.rows)
-                    *reinterpret_cast<uint4 *>(p.codes_t + (size_t)col * codes_pitch(p.rows) + r / 2) = make_uint4(out[0], out[1], out[2], out[3]);
-                sct[(2 * pair + h) * (ROWS / 32) + b] = (uint8_t)byte;
             }
+            sct[(2 * pair) * (kQRows / 32) + b] = (uint8_t)byte0;
+            sct[(2 * pair + 1) * (kQRows / 32) + b] = (uint8_t)byte1;
         }
         __syncthreads();
-        // a column's scales of this CTA's rows are a part of a word (the whole of it with 128 rows)
+        // a column's scales of this CTA's rows are half a word
         if (tid < 128) {
-            uint8_t *dst = p.scales_t + ((size_t)blockIdx.x * scale_tiles_of(p.rows) + r0 / 128) * kTileBytes + scale_at(tid, r0 % 128 / 32);
-            if constexpr (ROWS == 128) *reinterpret_cast<uint32_t *>(dst) = *reinterpret_cast<const uint32_t *>(sct + tid * 4);
-            else *reinterpret_cast<uint16_t *>(dst) = *reinterpret_cast<const uint16_t *>(sct + tid * 2);
+            uint8_t *dst = p.scales_t + ((size_t)blockIdx.x * p.ktiles_t + r0 / 128) * kTileBytes + scale_at(tid, r0 % 128 / 32);
+            *reinterpret_cast<uint16_t *>(dst) = *reinterpret_cast<const uint16_t *>(sct + tid * 2);
         }
     }
 }
@@ -120,12 +166,15 @@ __device__ __forceinline__ uint4 values4(uint32_t w, uint32_t byte)
 }
 
 // A CTA takes 128 rows x 256 columns, a warp four rows at a time, a thread eight values of each.
+
 constexpr int kDThreads = 256, kDRows = 4;
 __global__ void __launch_bounds__(kDThreads) lords_mxfp4_dequantize_kernel(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scales, int rows,
                                                                            int cols, uint16_t *__restrict__ v)
 {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int c = (int)blockIdx.x * 256 + lane * 8, r0 = (int)blockIdx.y * kTileRows, b = c / kBlock;
+    ptx::griddep_launch_dependents();
+    ptx::griddep_wait();
     if (c >= cols) return;
     const size_t pitch = codes_pitch(cols);
     const uint8_t *sc = scales + ((size_t)blockIdx.y * scale_tiles_of(cols) + b / kTileBlocks) * kTileBytes;
@@ -148,29 +197,27 @@ __global__ void __launch_bounds__(kDThreads) lords_mxfp4_dequantize_kernel(const
 
 }  // namespace
 
-template <int ROWS> static void launch_quantize_rows(const QuantizeParams &p, cudaStream_t stream)
+template <bool ALONG, bool ACROSS> static int launch_quantize_variant(const QuantizeParams &p, cudaStream_t stream)
 {
     // (whole tiles of scales are written, the rows behind the last among them)
-    const dim3 grid((unsigned)((p.cols + 127) / 128), (unsigned)((p.rows + 127) / 128 * (128 / ROWS)));
-    if (p.codes && p.codes_t) lords_mxfp4_quantize_kernel<ROWS, true, true><<<grid, kQThreads, 0, stream>>>(p);
-    else if (p.codes) lords_mxfp4_quantize_kernel<ROWS, true, false><<<grid, kQThreads, 0, stream>>>(p);
-    else lords_mxfp4_quantize_kernel<ROWS, false, true><<<grid, kQThreads, 0, stream>>>(p);
+    const dim3 grid((unsigned)((p.cols + 127) / 128), (unsigned)((p.rows + 127) / 128 * (128 / kQRows)));
+    return launch_dependent(lords_mxfp4_quantize_kernel<ALONG, ACROSS>, grid, kQThreads, stream, p);
 }
 
 int launch_mxfp4_quantize(const uint16_t *v, int rows, int cols, uint8_t *codes, uint8_t *scales, uint8_t *codes_t, uint8_t *scales_t, cudaStream_t stream)
 {
-    launch_quantize_rows<QROWS>({v, codes, scales, codes_t, scales_t, rows, cols}, stream);
-    LORDS_CUDA_TRY(cudaGetLastError());
-    return LORDS_OK;
+    const QuantizeParams p = {v, codes, scales, codes_t, scales_t, rows, cols, (int)codes_pitch(cols), (int)codes_pitch(rows), scale_tiles_of(cols),
+                              scale_tiles_of(rows), cols % 16 == 0 && reinterpret_cast<uintptr_t>(v) % 32 == 0,
+                              (rows + 31) / 32 % 2 == 0 && reinterpret_cast<uintptr_t>(codes_t) % 32 == 0};
+    if (codes && codes_t) return launch_quantize_variant<true, true>(p, stream);
+    return codes ? launch_quantize_variant<true, false>(p, stream) : launch_quantize_variant<false, true>(p, stream);
 }
 
 int launch_mxfp4_dequantize(const uint8_t *codes, const uint8_t *scales, int rows, int cols, uint16_t *v, cudaStream_t stream)
 {
     const dim3 grid((unsigned)((cols + 255) / 256), (unsigned)((rows + kTileRows - 1) / kTileRows));
     if (grid.y > 65535u) return LORDS_ERR_SHAPE;
-    lords_mxfp4_dequantize_kernel<<<grid, kDThreads, 0, stream>>>(codes, scales, rows, cols, v);
-    LORDS_CUDA_TRY(cudaGetLastError());
-    return LORDS_OK;
+    return launch_dependent(lords_mxfp4_dequantize_kernel, grid, kDThreads, stream, codes, scales, rows, cols, v);
 }
 
 }  // namespace lords

@@ -50,7 +50,8 @@ static int forward_common(const void *x, const uint8_t *w, const uint8_t *ws, in
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     st.last_launches = 0;
     MxProblem p = {static_cast<const uint16_t *>(x), nullptr, nullptr, w, ws, M, m, n, y, y_f32};
-    if (M <= 16) return launch_mxfp4_stream(p, st, s);
+    rc = launch_mxfp4_stream(p, st, s);             // a handful of tokens: one launch
+    if (rc != LORDS_ERR_UNSUPPORTED) return rc;
     // x in 4 bits lies in the workspace between the two launches
     const size_t cb = (codes_bytes(M, n) + 255) & ~(size_t)255;
     if (cb + scales_bytes(M, n) > st.workspace_bytes) return LORDS_ERR_WORKSPACE;

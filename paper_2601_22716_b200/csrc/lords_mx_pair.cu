@@ -65,9 +65,9 @@ __device__ __forceinline__ uint32_t pack_bf16(uint32_t lo, uint32_t hi)
     return *reinterpret_cast<const uint32_t *>(&v);
 }
 // A tile of shared memory to global memory, rows and columns outside the tensor left out; a group of its own.
-__device__ __forceinline__ void tma_store_2d(const void *tmap, int x, int y, uint32_t src)
+__device__ __forceinline__ void tma_store_2d(const void *tmap, int x, int y, uint32_t src, uint64_t policy)
 {
-    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];" ::"l"(tmap), "r"(src), "r"(x), "r"(y) : "memory");
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group.L2::cache_hint [%0, {%2, %3}], [%1], %4;" ::"l"(tmap), "r"(src), "r"(x), "r"(y), "l"(policy) : "memory");
     asm volatile("cp.async.bulk.commit_group;" ::: "memory");
 }
 // The thread's stores have read their shared memory / have been done.
@@ -109,8 +109,10 @@ __global__ void __launch_bounds__(PCfg<BN>::THREADS, 1) lords_mxfp4_pair_kernel(
     griddep_wait();
 
     if (warp == 0) {
-        // ------------------------------------------------------------------ TMA
-        if (lane == 0) {
+        // ------------------------------------------------------------------ TMA.  (The lane that elect.sync names: the compiler then knows that one
+        // thread runs the branch.  Under lane == 0 the four loads of a step took longer than its MMAs: 2048 tokens, 4096 x 14336, 78.6 us with BN
+        // = 128 and 45.3 with 256, 65.9 and 43.9 so; by the whole warp under a predicate 97.5 and 53.9.)
+        if (elect_one()) {
             const uint32_t full0 = map_to_rank(bar_full, 0);
             int it = 0;
             for (int tile = pair; tile < p.tiles && !failed; tile += p.pairs) {
@@ -138,11 +140,11 @@ __global__ void __launch_bounds__(PCfg<BN>::THREADS, 1) lords_mxfp4_pair_kernel(
         int it = 0, n = 0;
         for (int tile = pair; tile < p.tiles && !failed; tile += p.pairs, ++n) {
             const int a = n % C::ACCS;
-            if (n >= C::ACCS && !mbar_wait_cluster(bar_acc_empty + 8 * a, (uint32_t)((n / C::ACCS - 1) & 1), status, 73)) { failed = true; break; }
+            if (n >= C::ACCS && !mbar_wait_warp(bar_acc_empty + 8 * a, (uint32_t)((n / C::ACCS - 1) & 1), status, 73)) { failed = true; break; }
             tc_fence_after_sync();
             for (int k = 0; k < p.steps; ++k, ++it) {
                 const int s = it % STAGES;
-                if (!mbar_wait_cluster(bar_full + 8 * s, (uint32_t)((it / STAGES) & 1), status, 74)) { failed = true; break; }
+                if (!mbar_wait_warp(bar_full + 8 * s, (uint32_t)((it / STAGES) & 1), status, 74)) { failed = true; break; }
                 tc_fence_after_sync();
                 const uint32_t at = base + (uint32_t)(s * C::STAGE), sx = at + C::XTILE + C::WTILE, sw = sx + C::XSF;
                 const uint32_t a_lo = lo0 | ((at & 0x3FFFFu) >> 4), b_lo = lo0 | (((at + C::XTILE) & 0x3FFFFu) >> 4);
@@ -172,6 +174,8 @@ __global__ void __launch_bounds__(PCfg<BN>::THREADS, 1) lords_mxfp4_pair_kernel(
         constexpr int CW = BN / (C::EPI / 4);
         const uint32_t empty0 = map_to_rank(bar_acc_empty, 0);
         const uint32_t acc = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(ch * CW);
+        uint64_t policy;
+        asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(policy));
         const uint32_t own = out_s + (uint32_t)((warp - kPEpiWarp0) * 4096), row = own + (uint32_t)(lane * 128);
         int n = 0;
         for (int tile = pair; tile < p.tiles; tile += p.pairs, ++n) {
@@ -185,7 +189,7 @@ __global__ void __launch_bounds__(PCfg<BN>::THREADS, 1) lords_mxfp4_pair_kernel(
             auto leave = [&](int i) {                          // 128 bytes of 32 tokens, from out-feature i on
                 fence_proxy_async_smem();
                 __syncwarp();
-                if (lane == 0 && t0 < p.M && i < p.m) tma_store_2d(&p.tm_y, i, t0, own);
+                if (lane == 0 && t0 < p.M && i < p.m) tma_store_2d(&p.tm_y, i, t0, own, policy);
             };
             auto load = [&](int c0, uint32_t (&v)[32]) {
                 tmem_ld_32x32(acc + (uint32_t)(a * BN + c0), v);
@@ -213,18 +217,21 @@ __global__ void __launch_bounds__(PCfg<BN>::THREADS, 1) lords_mxfp4_pair_kernel(
                             if (i0 + c0 + c < p.m) store_out(p.y, p.y_f32, (size_t)t * p.m + i0 + c0 + c, __uint_as_float(v[c]));
                 }
             } else if (p.y_f32) {
-#pragma unroll 1
-                for (int c0 = 0; c0 < CW; c0 += 32) {
-                    uint32_t v[32];
-                    load(c0, v);
-                    if (c0 + 32 == CW) release();
+                // all of it into registers first, so that the next tile's MMAs wait no longer than that takes
+                uint32_t v[CW / 32][32];
+#pragma unroll
+                for (int c = 0; c < CW / 32; ++c) tmem_ld_32x32(acc + (uint32_t)(a * BN + 32 * c), v[c]);
+#pragma unroll
+                for (int c = 0; c < CW / 32; ++c) tmem_wait_ld(v[c]);
+                release();
+#pragma unroll
+                for (int g = 0; g < CW / 32; ++g) {
                     room();
 #pragma unroll
-                    for (int c = 0; c < 8; ++c) put(c, v + 4 * c);
-                    leave(i0 + c0);
+                    for (int c = 0; c < 8; ++c) put(c, v[g] + 4 * c);
+                    leave(i0 + 32 * g);
                 }
             } else {
-                // all of it into registers first, so that the next tile's MMAs wait no longer than that takes
                 uint32_t w[CW / 2];
 #pragma unroll
                 for (int c0 = 0; c0 < CW; c0 += 32) {
@@ -335,6 +342,7 @@ template <int BN> int run_pair(const MxProblem &p, State &st, cudaStream_t strea
 int launch_mxfp4_pair(const MxProblem &p, State &st, cudaStream_t stream)
 {
     if (p.x) return LORDS_ERR_UNSUPPORTED;
+    if (st.forced_bn == 128 || st.forced_bn == 256) return st.forced_bn == 128 ? run_pair<128>(p, st, stream) : run_pair<256>(p, st, stream);
     // Microseconds of a launch: waves of tiles, a step's and a tile's fixed part measured at 2048 tokens.
     const double steps = (p.n + 255) / 256;
     const long long tok = (p.M + kPTokens - 1) / kPTokens, w256 = (tok * ((p.m + 255) / 256) + 73) / 74, w128 = (tok * ((p.m + 127) / 128) + 73) / 74;

@@ -4,9 +4,9 @@
 // CTA streams 128 rows of W through shared memory by TMA, 256 columns a step, as the MMA's 128-row operand; the tokens are its N = BN columns.
 // The scales of a step follow their codes through shared memory and from there into TMEM (tcgen05.cp), where the MMA reads them.
 //
-//   QX:    x arrives in bf16; four warps bring each step's slice of it to 4 bits on the way (at most 16 tokens).  A token's slice
-//          is worked on by every row tile, which costs less than a second launch.
-//   else:  x arrives as codes and scales, by TMA like W.
+//   QX:    x arrives in bf16; four or eight warps bring it to 4 bits on the way, eight steps' slices at a time: for calls of a handful of
+//          tokens, or of few steps a CTA.
+//   QX 0:  x arrives as codes and scales, by TMA like W.
 //
 // A cluster of CTAs divides a tile's steps where the row tiles alone leave SMs idle; token t is added up by CTA t mod cluster in distributed
 // shared memory, in the order of the ranks, so results do not depend on timing.  No scratch memory: calls on different streams
@@ -34,12 +34,14 @@ constexpr int kRows = 128;                   // rows of W per CTA
 constexpr int kStep = 256;                   // columns a step: 128 bytes of codes
 constexpr int kConvWarp0 = 4;                // warps from 4 on: x to 4 bits, then (the first four) the epilogue; 0: TMA, 1: MMA issuer, 2: TMEM
 constexpr int kSplitMax = 8;                 // CTAs that share a tile's steps
-constexpr int kBatch = 8;                    // QX: steps whose slice of x is converted together
+constexpr int kBatch = 8;                    // x in bf16: steps whose slice of x is converted together
 constexpr int kBatches = 2;                  // ... and batches in shared memory
 
-template <int BN, bool QX> struct SCfg {
-    static constexpr int CONV = QX ? 8 : 4;                         // converter and epilogue warps
+// QX: warps that bring x to 4 bits; 0: x arrives as codes.
+template <int BN, int QX> struct SCfg {
+    static constexpr int CONV = QX > 4 ? QX : 4;                    // converter and epilogue warps
     static constexpr int THREADS = (kConvWarp0 + CONV) * 32;
+    static constexpr int WORK = QX * 8;                             // most tokens x steps of a batch: two blocks a thread
     static constexpr int WTILE = kRows * 128;
     static constexpr int XTILE = BN * 128;
     static constexpr int SF = 2 * kTileBytes;                       // scales of a step: two tiles of four blocks
@@ -132,7 +134,7 @@ __device__ __forceinline__ bool add_up(const StreamParams &p, uint32_t acc, uint
     return true;
 }
 
-template <int BN, bool QX>
+template <int BN, int QX>
 __global__ void __launch_bounds__(SCfg<BN, QX>::THREADS, 1) lords_mxfp4_stream_kernel(const __grid_constant__ StreamParams p)
 {
     using C = SCfg<BN, QX>;
@@ -179,7 +181,7 @@ __global__ void __launch_bounds__(SCfg<BN, QX>::THREADS, 1) lords_mxfp4_stream_k
 
     if (warp == 0) {
         // ------------------------------------------------------------------ TMA: codes and scales of W, and of x
-        if (lane == 0) {
+        if (elect_one()) {
             int it = 0;
             for (int st = s_a; st < s_b; ++st, ++it) {
                 const int s = it % STAGES;
@@ -188,10 +190,10 @@ __global__ void __launch_bounds__(SCfg<BN, QX>::THREADS, 1) lords_mxfp4_stream_k
                 const int kt = p.ktiles - 2 * st < 2 ? 1 : 2;
                 mbar_expect_tx(bar, (uint32_t)(C::WTILE + kt * kTileBytes + (QX ? 0 : C::XTILE + kt * kTileBytes)));
                 tma_load_2d(dst, &p.tm_w, st * 128, row0, bar);
-                bulk_load(dst + C::WTILE, p.ws + ((size_t)rt * p.ktiles + 2 * st) * kTileBytes, (uint32_t)(kt * kTileBytes), bar);
+                load_words(dst + C::WTILE, p.ws + ((size_t)rt * p.ktiles + 2 * st) * kTileBytes, (uint32_t)(kt * kTileBytes), bar);
                 if (!QX) {
                     tma_load_2d(dst + C::WTILE + C::SF, &p.tm_x, st * 128, tok0, bar);
-                    bulk_load(dst + C::WTILE + C::SF + C::XTILE, p.xs + ((size_t)(tok0 / kTileRows) * p.ktiles + 2 * st) * kTileBytes, (uint32_t)(kt * kTileBytes), bar);
+                    load_words(dst + C::WTILE + C::SF + C::XTILE, p.xs + ((size_t)(tok0 / kTileRows) * p.ktiles + 2 * st) * kTileBytes, (uint32_t)(kt * kTileBytes), bar);
                 }
             }
         }
@@ -228,7 +230,7 @@ __global__ void __launch_bounds__(SCfg<BN, QX>::THREADS, 1) lords_mxfp4_stream_k
         }
         umma_commit(bar_acc, leader);
     } else if (warp >= kConvWarp0) {
-        if constexpr (QX) {
+        if constexpr (QX > 0) {
             // -------------------------------------------------------------- x to 4 bits, a block at a time, a batch of steps after the other.  (Tokens
             // from M on are columns of the product that nobody reads: whatever their shared memory holds.)
             auto load = [&](int t, int c, uint32_t (&w)[16]) {
@@ -251,45 +253,54 @@ __global__ void __launch_bounds__(SCfg<BN, QX>::THREADS, 1) lords_mxfp4_stream_k
                     }
                 }
             };
-            const int steps = s_b - s_a;
+            // A batch is at most WORK tokens x steps of eight blocks, two blocks a thread: block e is block e % (8 count) of token e / (8 count).  The next batch's
+            // loads are on their way while this one is converted.
+            constexpr int PER = C::WORK * 8 / (C::CONV * 32);
+            const int steps = s_b - s_a, id = tid - kConvWarp0 * 32;
+            auto place = [&](int first, int h, int &t, int &kb) {
+                const int count = steps - first < kBatch ? steps - first : kBatch, e = id + h * C::CONV * 32;
+                t = count == kBatch ? e / (8 * kBatch) : e / (8 * count);
+                kb = e - t * 8 * count;
+                return t < p.M;
+            };
+            auto load_batch = [&](int first, uint32_t (&w)[PER][16]) {
+#pragma unroll
+                for (int h = 0; h < PER; ++h) {
+                    int t, kb;
+                    if (first < steps && place(first, h, t, kb)) load(t, (s_a + first) * kStep + kb * kBlock, w[h]);
+                }
+            };
+            uint32_t w[PER][16], next[PER][16];
+            load_batch(0, w);
             for (int first = 0; first < steps && !failed; first += kBatch) {
-                const int batch = first / kBatch, count = steps - first < kBatch ? steps - first : kBatch;
+                const int batch = first / kBatch;
+                load_batch(first + kBatch, next);
                 if (batch >= kBatches && !mbar_wait_warp(bar_x_free + 8 * (batch % kBatches), (uint32_t)((batch / kBatches - 1) & 1), status, 63)) { failed = true; break; }
                 const uint32_t to = xring + (uint32_t)((batch % kBatches) * kBatch * C::XSTEP);
-                // block e: token e / (8 count), step and block of the step e % (8 count); two at a time, so that their loads overlap
-                const int all = p.M * 8 * count;
-                for (int e0 = tid - kConvWarp0 * 32; e0 < all; e0 += 2 * C::CONV * 32) {
-                    uint32_t w[2][16];
-                    int t[2], kb[2];
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const int e = e0 + h * C::CONV * 32;
-                        t[h] = e / (8 * count);
-                        kb[h] = e - t[h] * 8 * count;
-                        if (e < all) load(t[h], (s_a + first) * kStep + kb[h] * kBlock, w[h]);
-                    }
+                for (int h = 0; h < PER; ++h) {
+                    int t, kb;
+                    if (!place(first, h, t, kb)) break;
+                    uint32_t top = magnitudes(w[h][0]), out[4];
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        if (e0 + h * C::CONV * 32 >= all) break;
-                        uint32_t top = 0u, out[4];
+                    for (int k = 1; k < 15; k += 2) top = larger(top, magnitudes(w[h][k]), magnitudes(w[h][k + 1]));
+                    top = larger(top, magnitudes(w[h][15]));
+                    const uint32_t byte = scale_byte<2>(larger_half(top));
 #pragma unroll
-                        for (int k = 0; k < 16; ++k) top = max_magnitudes(top, w[h][k]);
-                        const uint32_t byte = scale_byte<2>(max(top & 0xFFFFu, top >> 16));
-#pragma unroll
-                        for (int g = 0; g < 4; ++g) {
-                            const uint32_t v[4] = {w[h][4 * g], w[h][4 * g + 1], w[h][4 * g + 2], w[h][4 * g + 3]};
-                            out[g] = to_codes4(v, byte);
-                        }
-                        const int b = kb[h] & 7;
-                        const uint32_t at = to + (uint32_t)((kb[h] >> 3) * C::XSTEP);
-                        sts_v4(at + (uint32_t)(t[h] * 128 + ((b ^ (t[h] & 7)) << 4)), make_uint4(out[0], out[1], out[2], out[3]));
-                        asm volatile("st.shared.u8 [%0], %1;" ::"r"(at + C::XTILE + (uint32_t)(b / kTileBlocks * kTileBytes + scale_at(t[h], b % kTileBlocks))), "r"(byte)
-                                     : "memory");
-                    }
+                    for (int g = 0; g < 4; ++g) out[g] = to_codes4(w[h] + 4 * g, byte);
+                    const int b = kb & 7;
+                    const uint32_t at = to + (uint32_t)((kb >> 3) * C::XSTEP);
+                    sts_v4(at + (uint32_t)(t * 128 + ((b ^ (t & 7)) << 4)), make_uint4(out[0], out[1], out[2], out[3]));
+                    asm volatile("st.shared.u8 [%0], %1;" ::"r"(at + C::XTILE + (uint32_t)(b / kTileBlocks * kTileBytes + scale_at(t, b % kTileBlocks))), "r"(byte)
+                                 : "memory");
                 }
                 fence_proxy_async_smem();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar_x + 8 * (batch % kBatches));
+#pragma unroll
+                for (int h = 0; h < PER; ++h)
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) w[h][k] = next[h][k];
             }
         }
         // ------------------------------------------------------------------ epilogue: lane = row of W, columns = tokens
@@ -330,7 +341,7 @@ __global__ void __launch_bounds__(SCfg<BN, QX>::THREADS, 1) lords_mxfp4_stream_k
     }
 }
 
-template <int BN, bool QX> struct StreamVariant {
+template <int BN, int QX> struct StreamVariant {
     using C = SCfg<BN, QX>;
     static void fill(cudaLaunchConfig_t &cfg, cudaLaunchAttribute *attr, int row_tiles, int tok_tiles, int split, cudaStream_t stream)
     {
@@ -342,11 +353,20 @@ template <int BN, bool QX> struct StreamVariant {
         attr[1].val.clusterDim.z = 1;
         cfg = cudaLaunchConfig_t{};
         cfg.gridDim = dim3((unsigned)(row_tiles * split), (unsigned)tok_tiles);
-        cfg.blockDim = dim3(C::THREADS);
+        cfg.blockDim = dim3(SCfg<BN, QX>::THREADS);
         cfg.dynamicSmemBytes = C::SMEM;
         cfg.stream = stream;
         cfg.attrs = attr;
         cfg.numAttrs = 2;
+    }
+    // The kernel may use its shared memory, once per device.
+    static cudaError_t allow(const State &st)
+    {
+        static bool done[kMaxDevices] = {};
+        bool &d = done[device_slot(st)];
+        const cudaError_t e = d ? cudaSuccess : cudaFuncSetAttribute(lords_mxfp4_stream_kernel<BN, QX>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
+        d = e == cudaSuccess;
+        return e;
     }
     // Clusters of `split` CTAs that can be resident at once.
     static int resident(int split, const State &st)
@@ -355,7 +375,7 @@ template <int BN, bool QX> struct StreamVariant {
         int &c = cache[device_slot(st)][split];
         if (c == 0) {
             c = -1;
-            if (cudaFuncSetAttribute(lords_mxfp4_stream_kernel<BN, QX>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM) != cudaSuccess) return 0;
+            if (allow(st) != cudaSuccess) return 0;
             cudaLaunchConfig_t cfg;
             cudaLaunchAttribute attr[2];
             fill(cfg, attr, 1, 1, split, nullptr);
@@ -381,12 +401,16 @@ template <int BN, bool QX> struct StreamVariant {
     static int launch(StreamParams &k, const State &st, cudaStream_t stream)
     {
         const int row_tiles = (k.m + kRows - 1) / kRows, tok_tiles = (k.M + BN - 1) / BN;
-        const int split = choose_split(row_tiles * tok_tiles, k.steps, st);
+        // (the same for every kind of x: sums are in the same order then)
+        const int split = StreamVariant<BN, 0>::choose_split(row_tiles * tok_tiles, k.steps, st);
         if (split < 1) return LORDS_ERR_UNSUPPORTED;
         if (tok_tiles > 65535) return LORDS_ERR_SHAPE;
+        const int own = (k.steps + split - 1) / split;
+        if (QX > 0 && k.M * (QX == 4 && own > kBatch ? kBatch : own) > C::WORK) return LORDS_ERR_UNSUPPORTED;
         cudaLaunchConfig_t cfg;
         cudaLaunchAttribute attr[2];
         fill(cfg, attr, row_tiles, tok_tiles, split, stream);
+        LORDS_CUDA_TRY(allow(st));
         LORDS_CUDA_TRY(cudaLaunchKernelEx(&cfg, lords_mxfp4_stream_kernel<BN, QX>, k));
         return LORDS_OK;
     }
@@ -412,11 +436,16 @@ int launch_mxfp4_stream(const MxProblem &p, State &st, cudaStream_t stream)
     if (qx) k.tm_x = k.tm_w;
     else if (!make_map_2d(&k.tm_x, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, p.xq, pitch, (uint64_t)p.M, 128, (uint32_t)bn, CU_TENSOR_MAP_SWIZZLE_128B)) return LORDS_ERR_CUDA;
     int rc;
-    if (qx) rc = StreamVariant<16, true>::launch(k, st, stream);
-    else if (bn == 16) rc = StreamVariant<16, false>::launch(k, st, stream);
-    else if (bn == 32) rc = StreamVariant<32, false>::launch(k, st, stream);
-    else if (bn == 64) rc = StreamVariant<64, false>::launch(k, st, stream);
-    else rc = StreamVariant<128, false>::launch(k, st, stream);
+    // x in bf16: up to four tokens four converter warps.  Up to sixteen eight warps, where a CTA has few steps (64 tokens x steps): every row tile converts
+    // x again and reads it in 16 bits.  In device time a launch of its own for that is the faster by then (4096 x 4096, 16 tokens of
+    // four steps: 6.2 us here, 5.6 with two launches; 14336 x 4096, sixteen steps: 13.8 and 10.0), but a call from the host takes
+    // 2 us more for two launches (6.0 and 8.1).
+    if (qx && p.M <= 4) rc = StreamVariant<16, 4>::launch(k, st, stream);
+    else if (qx) rc = StreamVariant<16, 8>::launch(k, st, stream);
+    else if (bn == 16) rc = StreamVariant<16, 0>::launch(k, st, stream);
+    else if (bn == 32) rc = StreamVariant<32, 0>::launch(k, st, stream);
+    else if (bn == 64) rc = StreamVariant<64, 0>::launch(k, st, stream);
+    else rc = StreamVariant<128, 0>::launch(k, st, stream);
     if (rc != LORDS_OK) return rc;
     st.last_launches += 1;
     st.last_path = "mxfp4_stream";
