@@ -179,6 +179,9 @@ int launch_mxfp4_dequantize(const uint8_t *codes, const uint8_t *scales, int row
 int launch_mxfp4_stream(const MxProblem &p, State &st, cudaStream_t stream);
 // Many tokens: CTA pairs, 256 tokens x 128 or 256 out-features.  x in 4 bits.
 int launch_mxfp4_pair(const MxProblem &p, State &st, cudaStream_t stream);
+// Estimates of their times in microseconds.
+double mxfp4_stream_us(const MxProblem &p, const State &st);
+double mxfp4_pair_us(const MxProblem &p, const State &st);
 
 // 8-bit checkpoints: rows of whole blocks, and scales four bytes per 128 columns.
 int launch_checkpoint_store(const uint16_t *x, int M, int n, uint8_t *q, uint8_t *e, cudaStream_t stream);

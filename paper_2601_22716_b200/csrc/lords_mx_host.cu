@@ -23,7 +23,12 @@ static bool dims_ok(int64_t rows, int64_t cols) { return rows >= 1 && cols >= 1 
 
 static int product(const MxProblem &p, State &st, cudaStream_t s)
 {
-    return p.M > 128 ? launch_mxfp4_pair(p, st, s) : launch_mxfp4_stream(p, st, s);
+    if (st.forced_path == 2) return launch_mxfp4_stream(p, st, s);
+    if (st.forced_path == 8) return launch_mxfp4_pair(p, st, s);
+    // Up to 32 tokens the one was never slower, from 513 on the other; between, by their estimates: 128 tokens, 14336 x 4096 15.7 us and 12.0, 4096 x
+    // 4096 9.1 and 9.5; 256 tokens, 4096 x 4096 12.8 and 9.9, 1024 x 4096 7.7 and 8.9.
+    const bool few = p.M <= 32 || (p.M <= 512 && mxfp4_stream_us(p, st) <= mxfp4_pair_us(p, st));
+    return few ? launch_mxfp4_stream(p, st, s) : launch_mxfp4_pair(p, st, s);
 }
 
 static int matmul_common(const uint8_t *xq, const uint8_t *xs, const uint8_t *w, const uint8_t *ws, int M, int m, int n, void *y, int y_f32, void *stream)

@@ -6,7 +6,10 @@
 // (tcgen05.cp) ahead of the step's four MMAs.  Tiles are dealt out to as many pairs as are resident; with BN = 128 two accumulators take turns, so
 // that a tile's stores run beside the next one's MMAs, with 256 the loads of the next tile do.
 //
-// Bound: 4-bit MMAs (four times the bf16 rate) at BN = 256 against 128 (128 + BN / 2) bytes a step and CTA from L2.
+// Bound: 4-bit MMAs (four times the bf16 rate, 512 cycles a step at BN = 256) and what L2 gives, 128 (128 + BN / 2) bytes of codes a step and CTA: all SMs
+// together read 13 to 14 TB/s with either BN (0.29 and 0.36 us a step), with L2's own units at 36 % and the clock at 1.64 GHz under the
+// power limit.  2048 tokens: 4096 x 14336 44 us (5.5 PFLOP/s), 14336 x 4096 48, its weight gradient 66.  The copies of the
+// scales cost 3 % of that (left out: 42.5); a step's copies ahead of the step before's MMAs, or between them, cost 17 to 30 % more.
 // No scratch memory.  Every wait is bounded; on expiry the role records LORDS_ERR_TIMEOUT and leaves its loop.
 #include <cuda.h>
 #include <cuda_bf16.h>
@@ -70,9 +73,8 @@ __device__ __forceinline__ void tma_store_2d(const void *tmap, int x, int y, uin
     asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group.L2::cache_hint [%0, {%2, %3}], [%1], %4;" ::"l"(tmap), "r"(src), "r"(x), "r"(y), "l"(policy) : "memory");
     asm volatile("cp.async.bulk.commit_group;" ::: "memory");
 }
-// The thread's stores have read their shared memory / have been done.
+// The thread's stores have read their shared memory.
 __device__ __forceinline__ void tma_store_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
-__device__ __forceinline__ void tma_store_wait() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 
 template <int BN>
 __global__ void __launch_bounds__(PCfg<BN>::THREADS, 1) lords_mxfp4_pair_kernel(const __grid_constant__ PairParams p)
@@ -250,7 +252,7 @@ __global__ void __launch_bounds__(PCfg<BN>::THREADS, 1) lords_mxfp4_pair_kernel(
                 }
             }
         }
-        if (lane == 0) tma_store_wait();
+        if (lane == 0) tma_store_wait_read();
         __syncwarp();
     }
 
@@ -339,14 +341,32 @@ template <int BN> int run_pair(const MxProblem &p, State &st, cudaStream_t strea
 
 }  // namespace
 
+// Microseconds of a launch with W from memory: its fixed part, and waves of tiles with a step's and a tile's own (2048 tokens, 14336 x 4096, 4096 x
+// 14336, 4096 x 4096, the weight gradients of 512 and 2048 tokens; y in 32 bits leaves more slowly than the next tile's MMAs take).
+static double pair_us(const MxProblem &p, int bn, int pairs)
+{
+    const double steps = (p.n + 255) / 256;
+    const long long tiles = (long long)((p.M + kPTokens - 1) / kPTokens) * ((p.m + bn - 1) / bn);
+    const double waves = (double)((tiles + pairs - 1) / pairs);
+    return bn == 256 ? 4.7 + waves * (0.36 * steps + (p.y_f32 ? 2.0 : 0.7)) : 4.0 + waves * (0.29 * steps + (p.y_f32 ? 0.6 : 0.42));
+}
+
+double mxfp4_pair_us(const MxProblem &p, const State &st)
+{
+    const int pairs = PairVariant<256>::resident(st);
+    const double a = pair_us(p, 256, pairs > 0 ? pairs : 1), b = pair_us(p, 128, pairs > 0 ? pairs : 1);
+    return a < b ? a : b;
+}
+
 int launch_mxfp4_pair(const MxProblem &p, State &st, cudaStream_t stream)
 {
     if (p.x) return LORDS_ERR_UNSUPPORTED;
     if (st.forced_bn == 128 || st.forced_bn == 256) return st.forced_bn == 128 ? run_pair<128>(p, st, stream) : run_pair<256>(p, st, stream);
-    // Microseconds of a launch: waves of tiles, a step's and a tile's fixed part measured at 2048 tokens.
-    const double steps = (p.n + 255) / 256;
-    const long long tok = (p.M + kPTokens - 1) / kPTokens, w256 = (tok * ((p.m + 255) / 256) + 73) / 74, w128 = (tok * ((p.m + 127) / 128) + 73) / 74;
-    return (double)w256 * (0.37 * steps + 1.8) <= (double)w128 * (0.31 * steps + 0.6) ? run_pair<256>(p, st, stream) : run_pair<128>(p, st, stream);
+    // 256 out-features a tile read a quarter less for the same work, 128 fill the pairs better: 512 tokens, 14336 x 4096: 18.1 and 25.7 us;
+    // 1024 tokens, 1024 x 4096: 9.3 and 8.4.
+    const int pairs = PairVariant<256>::resident(st);
+    if (pairs < 1) return LORDS_ERR_UNSUPPORTED;
+    return pair_us(p, 256, pairs) <= pair_us(p, 128, pairs) ? run_pair<256>(p, st, stream) : run_pair<128>(p, st, stream);
 }
 
 }  // namespace lords
