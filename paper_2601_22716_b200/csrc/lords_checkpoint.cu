@@ -83,18 +83,17 @@ __global__ void __launch_bounds__(kCThreads) lords_checkpoint_load_kernel(const 
     const int c = (int)blockIdx.x * 256 + lane * 8;
     ptx::griddep_launch_dependents();
     ptx::griddep_wait();
-    if (c >= n) return;
     uint2 w[PER];
     uint32_t byte[PER];
 #pragma unroll
     for (int k = 0; k < PER; ++k) {
-        const int t = t0 + k < M ? t0 + k : M - 1;
-        w[k] = __ldg(reinterpret_cast<const uint2 *>(q + (size_t)t * qp + c));
-        byte[k] = __ldg(e + (size_t)t * ep + c / kBlock);
+        const bool in = t0 + k < M && c < n;
+        w[k] = in ? __ldg(reinterpret_cast<const uint2 *>(q + (size_t)(t0 + k) * qp + c)) : make_uint2(0u, 0u);
+        byte[k] = in ? __ldg(e + (size_t)(t0 + k) * ep + c / kBlock) : 0u;
     }
 #pragma unroll
     for (int k = 0; k < PER; ++k)
-        if (t0 + k < M) store8(x + (size_t)(t0 + k) * n, n, c, values8(w[k], byte[k]));
+        if (t0 + k < M) store8(x + (size_t)(t0 + k) * n, n, c, values8(w[k], byte[k]), lane);
 }
 
 // One row a warp where four would leave fewer than two CTAs an SM.

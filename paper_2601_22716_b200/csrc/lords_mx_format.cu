@@ -165,34 +165,27 @@ __device__ __forceinline__ uint4 values4(uint32_t w, uint32_t byte)
     return make_uint4(__byte_perm(v[0], v[1], 0x5410), __byte_perm(v[2], v[3], 0x5410), __byte_perm(v[0], v[1], 0x7632), __byte_perm(v[2], v[3], 0x7632));
 }
 
-// A CTA takes 128 rows x 256 columns, a warp four rows at a time, a thread eight values of each.
-
+// A CTA takes 32 rows x 256 columns, a warp four rows, a thread eight values of each.  (128 rows, four after four: 2048 x 4096 9.2 us, 14336 x 4096 28.)
 constexpr int kDThreads = 256, kDRows = 4;
 __global__ void __launch_bounds__(kDThreads) lords_mxfp4_dequantize_kernel(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scales, int rows,
-                                                                           int cols, uint16_t *__restrict__ v)
+                                                                           int cols, int pitch, int ktiles, uint16_t *__restrict__ v)
 {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int c = (int)blockIdx.x * 256 + lane * 8, r0 = (int)blockIdx.y * kTileRows, b = c / kBlock;
+    const int c = (int)blockIdx.x * 256 + lane * 8, r0 = ((int)blockIdx.y * (kDThreads / 32) + warp) * kDRows, b = c / kBlock;
     ptx::griddep_launch_dependents();
     ptx::griddep_wait();
-    if (c >= cols) return;
-    const size_t pitch = codes_pitch(cols);
-    const uint8_t *sc = scales + ((size_t)blockIdx.y * scale_tiles_of(cols) + b / kTileBlocks) * kTileBytes;
-#pragma unroll 1
-    for (int r = warp * kDRows; r < kTileRows && r0 + r < rows; r += kDThreads / 32 * kDRows) {
-        uint32_t w[kDRows], e[kDRows];
+    // (the four rows lie in one row of tiles)
+    const uint8_t *sc = scales + ((size_t)(r0 / kTileRows) * ktiles + b / kTileBlocks) * kTileBytes;
+    uint32_t w[kDRows], e[kDRows];
 #pragma unroll
-        for (int k = 0; k < kDRows; ++k) {
-            const bool in = r0 + r + k < rows;
-            w[k] = in ? __ldg(reinterpret_cast<const uint32_t *>(codes + (size_t)(r0 + r + k) * pitch + c / 2)) : 0u;
-            e[k] = __ldg(sc + scale_at(r + k, b % kTileBlocks));
-        }
-#pragma unroll
-        for (int k = 0; k < kDRows; ++k) {
-            if (r0 + r + k >= rows) break;
-            store8(v + (size_t)(r0 + r + k) * cols, cols, c, values4(w[k], e[k]));
-        }
+    for (int k = 0; k < kDRows; ++k) {
+        const bool in = r0 + k < rows && c < cols;
+        w[k] = in ? __ldg(reinterpret_cast<const uint32_t *>(codes + (size_t)(r0 + k) * pitch + c / 2)) : 0u;
+        e[k] = in ? __ldg(sc + scale_at((r0 + k) % kTileRows, b % kTileBlocks)) : 0u;
     }
+#pragma unroll
+    for (int k = 0; k < kDRows; ++k)
+        if (r0 + k < rows) store8(v + (size_t)(r0 + k) * cols, cols, c, values4(w[k], e[k]), lane);
 }
 
 }  // namespace
@@ -215,9 +208,9 @@ int launch_mxfp4_quantize(const uint16_t *v, int rows, int cols, uint8_t *codes,
 
 int launch_mxfp4_dequantize(const uint8_t *codes, const uint8_t *scales, int rows, int cols, uint16_t *v, cudaStream_t stream)
 {
-    const dim3 grid((unsigned)((cols + 255) / 256), (unsigned)((rows + kTileRows - 1) / kTileRows));
-    if (grid.y > 65535u) return LORDS_ERR_SHAPE;
-    return launch_dependent(lords_mxfp4_dequantize_kernel, grid, kDThreads, stream, codes, scales, rows, cols, v);
+    constexpr int per = kDThreads / 32 * kDRows;
+    const dim3 grid((unsigned)((cols + 255) / 256), (unsigned)((rows + per - 1) / per));
+    return launch_dependent(lords_mxfp4_dequantize_kernel, grid, kDThreads, stream, codes, scales, rows, cols, (int)codes_pitch(cols), scale_tiles_of(cols), v);
 }
 
 }  // namespace lords

@@ -184,14 +184,36 @@ __global__ void __launch_bounds__(PCfg<BN>::THREADS, 1) lords_mxfp4_pair_kernel(
             const int a = n % C::ACCS, wt = tile / p.tok_tiles, tt = tile - wt * p.tok_tiles;
             if (!__all_sync(0xffffffffu, mbar_wait_cluster(bar_acc_full + 8 * a, (uint32_t)((n / C::ACCS) & 1), status, 75))) { failed = true; break; }
             tc_fence_after_sync();
-            const int t0 = tt * kPTokens + rank * 128 + q * 32, t = t0 + lane;
+            const int t0 = tt * kPTokens + rank * 128 + q * 32;
             auto put = [&](int c, const uint32_t *w) {        // 16 bytes of the thread's row, chunk c of 8
                 sts_v4(row + (uint32_t)((c ^ (lane & 7)) << 4), make_uint4(w[0], w[1], w[2], w[3]));
             };
             auto leave = [&](int i) {                          // 128 bytes of 32 tokens, from out-feature i on
-                fence_proxy_async_smem();
+                if (p.y_by_tma) {
+                    fence_proxy_async_smem();
+                    __syncwarp();
+                    if (lane == 0 && t0 < p.M && i < p.m) tma_store_2d(&p.tm_y, i, t0, own, policy);
+                    return;
+                }
+                // rows of y that TMA cannot express: token after token, the warp's lanes side by side (2048 tokens, 4094 x 4096: 88 us when every lane
+                // stored its own token's values)
                 __syncwarp();
-                if (lane == 0 && t0 < p.M && i < p.m) tma_store_2d(&p.tm_y, i, t0, own, policy);
+                const int count = p.M - t0 < 32 ? p.M - t0 : 32;
+                for (int r = 0; r < count; ++r) {
+                    auto at = [&](int byte) { return own + (uint32_t)(r * 128 + (((byte >> 4) ^ (r & 7)) << 4) + (byte & 15)); };
+                    const size_t to = (size_t)(t0 + r) * p.m + i;
+                    if (p.y_f32) {
+                        if (i + lane < p.m) static_cast<uint32_t *>(p.y)[to + lane] = lds_u32(at(4 * lane));
+                    } else if ((p.m & 1) == 0) {
+                        if (i + 2 * lane < p.m) *reinterpret_cast<uint32_t *>(static_cast<uint16_t *>(p.y) + to + 2 * lane) = lds_u32(at(4 * lane));
+                    } else {
+                        const uint32_t two = lds_u32(at(4 * lane));
+                        uint16_t *dst = static_cast<uint16_t *>(p.y) + to + 2 * lane;
+                        if (i + 2 * lane < p.m) dst[0] = (uint16_t)two;
+                        if (i + 2 * lane + 1 < p.m) dst[1] = (uint16_t)(two >> 16);
+                    }
+                }
+                __syncwarp();
             };
             auto load = [&](int c0, uint32_t (&v)[32]) {
                 tmem_ld_32x32(acc + (uint32_t)(a * BN + c0), v);
@@ -203,22 +225,11 @@ __global__ void __launch_bounds__(PCfg<BN>::THREADS, 1) lords_mxfp4_pair_kernel(
                 if (lane == 0) mbar_arrive_pair(empty0 + 8 * a);
             };
             auto room = [&]() {                                // what left last has been read from the warp's tile
-                if (lane == 0) tma_store_wait_read();
+                if (p.y_by_tma && lane == 0) tma_store_wait_read();
                 __syncwarp();
             };
             const int i0 = wt * BN + ch * CW;
-            if (!p.y_by_tma) {
-#pragma unroll 1
-                for (int c0 = 0; c0 < CW; c0 += 32) {
-                    uint32_t v[32];
-                    load(c0, v);
-                    if (c0 + 32 == CW) release();
-                    if (t < p.M)
-#pragma unroll
-                        for (int c = 0; c < 32; ++c)
-                            if (i0 + c0 + c < p.m) store_out(p.y, p.y_f32, (size_t)t * p.m + i0 + c0 + c, __uint_as_float(v[c]));
-                }
-            } else if (p.y_f32) {
+            if (p.y_f32) {
                 // all of it into registers first, so that the next tile's MMAs wait no longer than that takes
                 uint32_t v[CW / 32][32];
 #pragma unroll
