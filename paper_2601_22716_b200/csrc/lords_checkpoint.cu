@@ -14,36 +14,49 @@ namespace {
 using namespace mx;
 
 constexpr int kCThreads = 256;
+constexpr int kStoreRows = 2;               // rows a warp of the store (four: 2048 x 4096 6.0 us, two 5.4)
 
-// A CTA takes eight warps' rows x 256 columns: a warp PER rows, a thread eight values of each.  Small calls take one row a warp and more CTAs.
+// A CTA takes eight warps' rows x 512 columns: a warp PER rows, a thread sixteen values of each, so that two threads are a block.  Small calls take one
+// row a warp and more CTAs.  (Eight values a thread: 2048 x 4096 6.6 us.)
 template <int PER>
-__global__ void __launch_bounds__(kCThreads) lords_checkpoint_store_kernel(const uint16_t *__restrict__ x, int M, int n, int qp, int ep, uint8_t *__restrict__ q,
-                                                                           uint8_t *__restrict__ e)
+__global__ void __launch_bounds__(kCThreads) lords_checkpoint_store_kernel(const uint16_t *x, int M, int n, int qp, int ep, int wide, uint8_t *q, uint8_t *e)
 {
     const int lane = threadIdx.x & 31, t0 = ((int)blockIdx.y * (kCThreads / 32) + (threadIdx.x >> 5)) * PER;
-    const int c = (int)blockIdx.x * 256 + lane * 8;
+    const int c = (int)blockIdx.x * 512 + lane * 16;
     const uint16_t *end = x + (size_t)M * n;
     ptx::griddep_launch_dependents();
     ptx::griddep_wait();
-    uint32_t w[PER][4];
+    uint32_t w[PER][8];
 #pragma unroll
     for (int k = 0; k < PER; ++k) {
-        w[k][0] = w[k][1] = w[k][2] = w[k][3] = 0u;
-        if (t0 + k < M && c < n) load8(x + (size_t)(t0 + k) * n, n, c, end, w[k]);
+#pragma unroll
+        for (int h = 0; h < 8; ++h) w[k][h] = 0u;
+        if (t0 + k >= M || c >= n) continue;
+        const uint16_t *row = x + (size_t)(t0 + k) * n;
+        if (wide) {
+            asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                         : "=r"(w[k][0]), "=r"(w[k][1]), "=r"(w[k][2]), "=r"(w[k][3]), "=r"(w[k][4]), "=r"(w[k][5]), "=r"(w[k][6]), "=r"(w[k][7])
+                         : "l"(row + c));
+        } else {
+            load8(row, n, c, end, w[k]);
+            if (c + 8 < n) load8(row, n, c + 8, end, w[k] + 4);
+        }
     }
 #pragma unroll
     for (int k = 0; k < PER; ++k) {
-        uint32_t top = larger(larger(magnitudes(w[k][0]), magnitudes(w[k][1]), magnitudes(w[k][2])), magnitudes(w[k][3]));
+        uint32_t top = larger(magnitudes(w[k][0]), magnitudes(w[k][1]), magnitudes(w[k][2]));
+        top = larger(top, magnitudes(w[k][3]), magnitudes(w[k][4]));
+        top = larger(top, magnitudes(w[k][5]), magnitudes(w[k][6]));
+        top = larger(top, magnitudes(w[k][7]));
         top = larger(top, __shfl_xor_sync(0xffffffffu, top, 1));
-        top = larger(top, __shfl_xor_sync(0xffffffffu, top, 2));
         const uint32_t byte = scale_byte<0>(larger_half(top));
         if (t0 + k >= M) continue;
         // value * 2^-E is exact in bf16; limited to 127/64 (which takes no more than half a step: the largest bf16 number below 2 is 127.5/64), then
         // times 64 onto 1.5 * 2^23, whose low bits are then the whole number: one rounding, ties to even
         const uint32_t inv = inverse_scale(byte);
-        uint32_t out[2];
+        uint32_t out[4];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
+        for (int h = 0; h < 4; ++h) {
             uint32_t u[2];
 #pragma unroll
             for (int g = 0; g < 2; ++g) {
@@ -52,10 +65,10 @@ __global__ void __launch_bounds__(kCThreads) lords_checkpoint_store_kernel(const
             }
             auto whole = [](float v) { return __float_as_uint(fmaf(v, 64.0f, 12582912.0f)); };
             out[h] = __byte_perm(__byte_perm(whole(low_half(u[0])), whole(high_half(u[0])), 0x0040), __byte_perm(whole(low_half(u[1])), whole(high_half(u[1])), 0x0040), 0x5410);
+            if (byte == 255u) out[h] = 0u;
         }
-        if (byte == 255u) out[0] = out[1] = 0u;
-        if (c < qp) *reinterpret_cast<uint2 *>(q + (size_t)(t0 + k) * qp + c) = make_uint2(out[0], out[1]);
-        if ((lane & 3) == 0 && c / kBlock < ep) e[(size_t)(t0 + k) * ep + c / kBlock] = (uint8_t)byte;
+        if (c < qp) *reinterpret_cast<uint4 *>(q + (size_t)(t0 + k) * qp + c) = make_uint4(out[0], out[1], out[2], out[3]);
+        if ((lane & 1) == 0 && c / kBlock < ep) e[(size_t)(t0 + k) * ep + c / kBlock] = (uint8_t)byte;
     }
 }
 
@@ -76,8 +89,8 @@ __device__ __forceinline__ uint4 values8(uint2 q, uint32_t byte)
 }
 
 template <int PER>
-__global__ void __launch_bounds__(kCThreads) lords_checkpoint_load_kernel(const uint8_t *__restrict__ q, const uint8_t *__restrict__ e, int M, int n, int qp, int ep,
-                                                                          uint16_t *__restrict__ x)
+__global__ void __launch_bounds__(kCThreads) lords_checkpoint_load_kernel(const uint8_t *q, const uint8_t *e, int M, int n, int qp, int ep,
+                                                                          uint16_t *x)
 {
     const int lane = threadIdx.x & 31, t0 = ((int)blockIdx.y * (kCThreads / 32) + (threadIdx.x >> 5)) * PER;
     const int c = (int)blockIdx.x * 256 + lane * 8;
@@ -88,32 +101,33 @@ __global__ void __launch_bounds__(kCThreads) lords_checkpoint_load_kernel(const 
 #pragma unroll
     for (int k = 0; k < PER; ++k) {
         const bool in = t0 + k < M && c < n;
-        w[k] = in ? __ldg(reinterpret_cast<const uint2 *>(q + (size_t)(t0 + k) * qp + c)) : make_uint2(0u, 0u);
-        byte[k] = in ? __ldg(e + (size_t)(t0 + k) * ep + c / kBlock) : 0u;
+        w[k] = in ? *reinterpret_cast<const uint2 *>(q + (size_t)(t0 + k) * qp + c) : make_uint2(0u, 0u);
+        byte[k] = in ? (uint32_t)e[(size_t)(t0 + k) * ep + c / kBlock] : 0u;
     }
 #pragma unroll
     for (int k = 0; k < PER; ++k)
         if (t0 + k < M) store8(x + (size_t)(t0 + k) * n, n, c, values8(w[k], byte[k]), lane);
 }
 
-// One row a warp where four would leave fewer than two CTAs an SM.
-bool small(int M, int n) { return (long long)((M + 31) / 32) * ((n + 255) / 256) < 296; }
-dim3 grid_of(int M, int cols, int per) { return dim3((unsigned)((cols + 255) / 256), (unsigned)((M + 8 * per - 1) / (8 * per))); }
+// One row a warp where more would leave fewer than two CTAs an SM.
+bool small(int M, int n, int cols, int per) { return (long long)((M + 8 * per - 1) / (8 * per)) * ((n + cols - 1) / cols) < 296; }
+dim3 grid_of(int M, int n, int cols, int per) { return dim3((unsigned)((n + cols - 1) / cols), (unsigned)((M + 8 * per - 1) / (8 * per))); }
 
 }  // namespace
 
 int launch_checkpoint_store(const uint16_t *x, int M, int n, uint8_t *q, uint8_t *e, cudaStream_t stream)
 {
     const int qp = blocks_of(n) * kBlock, ep = scale_tiles_of(n) * kTileBlocks;       // (whole words of scales are written)
-    if (small(M, n)) return launch_dependent(lords_checkpoint_store_kernel<1>, grid_of(M, ep * kBlock, 1), kCThreads, stream, x, M, n, qp, ep, q, e);
-    return launch_dependent(lords_checkpoint_store_kernel<4>, grid_of(M, ep * kBlock, 4), kCThreads, stream, x, M, n, qp, ep, q, e);
+    const int wide = n % 16 == 0 && reinterpret_cast<uintptr_t>(x) % 32 == 0;
+    if (small(M, n, 512, kStoreRows)) return launch_dependent(lords_checkpoint_store_kernel<1>, grid_of(M, ep * kBlock, 512, 1), kCThreads, stream, x, M, n, qp, ep, wide, q, e);
+    return launch_dependent(lords_checkpoint_store_kernel<kStoreRows>, grid_of(M, ep * kBlock, 512, kStoreRows), kCThreads, stream, x, M, n, qp, ep, wide, q, e);
 }
 
 int launch_checkpoint_load(const uint8_t *q, const uint8_t *e, int M, int n, uint16_t *x, cudaStream_t stream)
 {
     const int qp = blocks_of(n) * kBlock, ep = scale_tiles_of(n) * kTileBlocks;
-    if (small(M, n)) return launch_dependent(lords_checkpoint_load_kernel<1>, grid_of(M, n, 1), kCThreads, stream, q, e, M, n, qp, ep, x);
-    return launch_dependent(lords_checkpoint_load_kernel<4>, grid_of(M, n, 4), kCThreads, stream, q, e, M, n, qp, ep, x);
+    if (small(M, n, 256, 4)) return launch_dependent(lords_checkpoint_load_kernel<1>, grid_of(M, n, 256, 1), kCThreads, stream, q, e, M, n, qp, ep, x);
+    return launch_dependent(lords_checkpoint_load_kernel<4>, grid_of(M, n, 256, 4), kCThreads, stream, q, e, M, n, qp, ep, x);
 }
 
 }  // namespace lords

@@ -41,19 +41,33 @@ __device__ __forceinline__ uint32_t bf16x2_mul(uint32_t a, uint32_t b)
     return d;
 }
 
-// Eight values of a row of `cols` from column c (below cols) on, as pairs, zeros behind the last.  `end`: behind the matrix.
-__device__ __forceinline__ void load8(const uint16_t *__restrict__ row, int cols, int c, const uint16_t *end, uint32_t *w)
+// Eight values of a row of `cols` from column c (below cols) on, as pairs, zeros behind the last.  `end`: behind the matrix.  (Ordinary loads: a
+// dependent launch reads what another grid has written while it was already there, which the read-only path does not allow for.)
+__device__ __forceinline__ void load8(const uint16_t *row, int cols, int c, const uint16_t *end, uint32_t *w)
 {
     const uint16_t *src = row + c;
     if ((cols & 7) == 0) {
-        const uint4 q = __ldg(reinterpret_cast<const uint4 *>(src));
+        const uint4 q = *reinterpret_cast<const uint4 *>(src);
         w[0] = q.x; w[1] = q.y; w[2] = q.z; w[3] = q.w;
         return;
     }
-    load_words_anywhere<4>(reinterpret_cast<const uint8_t *>(src), reinterpret_cast<const uint8_t *>(end), w);
+    // the aligned words around; one that reaches past the end is read by halves
+    const bool between = (reinterpret_cast<uintptr_t>(src) & 2) != 0;
+    const uint16_t *at = src - (between ? 1 : 0);
+    uint32_t v[5];
+#pragma unroll
+    for (int k = 0; k < 5; ++k) {
+        v[k] = 0u;
+        if (k == 4 && !between) continue;
+        if (at + 2 * k + 2 <= end) v[k] = *reinterpret_cast<const uint32_t *>(at + 2 * k);
+        else if (at + 2 * k < end) v[k] = at[2 * k];
+    }
     const int left = cols - c;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) w[k] = left >= 2 * k + 2 ? w[k] : left > 2 * k ? w[k] & 0xFFFFu : 0u;
+    for (int k = 0; k < 4; ++k) {
+        const uint32_t u = between ? __funnelshift_r(v[k], v[k + 1], 16) : v[k];
+        w[k] = left >= 2 * k + 2 ? u : left > 2 * k ? u & 0xFFFFu : 0u;
+    }
 }
 // ... and to a row: a warp's lanes side by side, lane l from column c = c(0) + 8 l on; all 32 take part, those from column `cols` on store nothing.
 // Rows that begin between two words: every lane stores its neighbour's last value with its own first ones, as whole words (byte by byte

@@ -54,7 +54,7 @@ template <bool ALONG, bool ACROSS> __global__ void __launch_bounds__(kQThreads) 
         if (i >= p.rows) continue;
         if (p.wide) {
             if (c < p.cols)
-                asm volatile("ld.global.nc.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
                              : "=r"(w[k][0]), "=r"(w[k][1]), "=r"(w[k][2]), "=r"(w[k][3]), "=r"(w[k][4]), "=r"(w[k][5]), "=r"(w[k][6]), "=r"(w[k][7])
                              : "l"(src));
         } else {
@@ -167,8 +167,8 @@ __device__ __forceinline__ uint4 values4(uint32_t w, uint32_t byte)
 
 // A CTA takes 32 rows x 256 columns, a warp four rows, a thread eight values of each.  (128 rows, four after four: 2048 x 4096 9.2 us, 14336 x 4096 28.)
 constexpr int kDThreads = 256, kDRows = 4;
-__global__ void __launch_bounds__(kDThreads) lords_mxfp4_dequantize_kernel(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scales, int rows,
-                                                                           int cols, int pitch, int ktiles, uint16_t *__restrict__ v)
+__global__ void __launch_bounds__(kDThreads) lords_mxfp4_dequantize_kernel(const uint8_t *codes, const uint8_t *scales, int rows,
+                                                                           int cols, int pitch, int ktiles, uint16_t *v)
 {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int c = (int)blockIdx.x * 256 + lane * 8, r0 = ((int)blockIdx.y * (kDThreads / 32) + warp) * kDRows, b = c / kBlock;
@@ -180,8 +180,8 @@ __global__ void __launch_bounds__(kDThreads) lords_mxfp4_dequantize_kernel(const
 #pragma unroll
     for (int k = 0; k < kDRows; ++k) {
         const bool in = r0 + k < rows && c < cols;
-        w[k] = in ? __ldg(reinterpret_cast<const uint32_t *>(codes + (size_t)(r0 + k) * pitch + c / 2)) : 0u;
-        e[k] = in ? __ldg(sc + scale_at((r0 + k) % kTileRows, b % kTileBlocks)) : 0u;
+        w[k] = in ? *reinterpret_cast<const uint32_t *>(codes + (size_t)(r0 + k) * pitch + c / 2) : 0u;
+        e[k] = in ? sc[scale_at((r0 + k) % kTileRows, b % kTileBlocks)] : 0u;
     }
 #pragma unroll
     for (int k = 0; k < kDRows; ++k)
