@@ -88,25 +88,43 @@ __device__ __forceinline__ uint4 values8(uint2 q, uint32_t byte)
     return make_uint4(v[0], v[1], v[2], v[3]);
 }
 
-template <int PER>
-__global__ void __launch_bounds__(kCThreads) lords_checkpoint_load_kernel(const uint8_t *q, const uint8_t *e, int M, int n, int qp, int ep,
-                                                                          uint16_t *x)
+// A warp takes PER rows x 256 columns, a thread eight values of each; WIDE, rows that begin at 32-byte boundaries: 512 columns, sixteen values.
+template <int PER, bool WIDE>
+__global__ void __launch_bounds__(kCThreads) lords_checkpoint_load_kernel(const uint8_t *q, const uint8_t *e, int M, int n, int qp, int ep, uint16_t *x)
 {
+    constexpr int VALUES = WIDE ? 16 : 8;
     const int lane = threadIdx.x & 31, t0 = ((int)blockIdx.y * (kCThreads / 32) + (threadIdx.x >> 5)) * PER;
-    const int c = (int)blockIdx.x * 256 + lane * 8;
+    const int c = ((int)blockIdx.x * 32 + lane) * VALUES;
     ptx::griddep_launch_dependents();
     ptx::griddep_wait();
-    uint2 w[PER];
+    uint2 w[PER][VALUES / 8];
     uint32_t byte[PER];
 #pragma unroll
     for (int k = 0; k < PER; ++k) {
-        const bool in = t0 + k < M && c < n;
-        w[k] = in ? *reinterpret_cast<const uint2 *>(q + (size_t)(t0 + k) * qp + c) : make_uint2(0u, 0u);
-        byte[k] = in ? (uint32_t)e[(size_t)(t0 + k) * ep + c / kBlock] : 0u;
+        byte[k] = 0u;
+#pragma unroll
+        for (int h = 0; h < VALUES / 8; ++h) w[k][h] = make_uint2(0u, 0u);
+        if (t0 + k >= M || c >= n) continue;
+        const uint8_t *src = q + (size_t)(t0 + k) * qp + c;
+        if constexpr (WIDE) {
+            const uint4 u = *reinterpret_cast<const uint4 *>(src);
+            w[k][0] = make_uint2(u.x, u.y);
+            w[k][1] = make_uint2(u.z, u.w);
+        } else {
+            w[k][0] = *reinterpret_cast<const uint2 *>(src);
+        }
+        byte[k] = e[(size_t)(t0 + k) * ep + c / kBlock];
     }
 #pragma unroll
-    for (int k = 0; k < PER; ++k)
-        if (t0 + k < M) store8(x + (size_t)(t0 + k) * n, n, c, values8(w[k], byte[k]), lane);
+    for (int k = 0; k < PER; ++k) {
+        if (t0 + k >= M) break;
+        uint16_t *row = x + (size_t)(t0 + k) * n;
+        if constexpr (WIDE) {
+            if (c < n) store16(row + c, values8(w[k][0], byte[k]), values8(w[k][1], byte[k]));
+        } else {
+            store8(row, n, c, values8(w[k][0], byte[k]), lane);
+        }
+    }
 }
 
 // One row a warp where more would leave fewer than two CTAs an SM.
@@ -126,8 +144,10 @@ int launch_checkpoint_store(const uint16_t *x, int M, int n, uint8_t *q, uint8_t
 int launch_checkpoint_load(const uint8_t *q, const uint8_t *e, int M, int n, uint16_t *x, cudaStream_t stream)
 {
     const int qp = blocks_of(n) * kBlock, ep = scale_tiles_of(n) * kTileBlocks;
-    if (small(M, n, 256, 4)) return launch_dependent(lords_checkpoint_load_kernel<1>, grid_of(M, n, 256, 1), kCThreads, stream, q, e, M, n, qp, ep, x);
-    return launch_dependent(lords_checkpoint_load_kernel<4>, grid_of(M, n, 256, 4), kCThreads, stream, q, e, M, n, qp, ep, x);
+    auto launch = [&](auto kernel, int cols, int per) { return launch_dependent(kernel, grid_of(M, n, cols, per), kCThreads, stream, q, e, M, n, qp, ep, x); };
+    if (n % 16 == 0 && reinterpret_cast<uintptr_t>(x) % 32 == 0)
+        return small(M, n, 512, 2) ? launch(lords_checkpoint_load_kernel<1, true>, 512, 1) : launch(lords_checkpoint_load_kernel<2, true>, 512, 2);
+    return small(M, n, 256, 4) ? launch(lords_checkpoint_load_kernel<1, false>, 256, 1) : launch(lords_checkpoint_load_kernel<4, false>, 256, 4);
 }
 
 }  // namespace lords

@@ -69,6 +69,12 @@ __device__ __forceinline__ void load8(const uint16_t *row, int cols, int c, cons
         w[k] = left >= 2 * k + 2 ? u : left > 2 * k ? u & 0xFFFFu : 0u;
     }
 }
+// Sixteen values to a 32-byte boundary: whole sectors.
+__device__ __forceinline__ void store16(uint16_t *dst, uint4 a, uint4 b)
+{
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(dst), "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b.x), "r"(b.y), "r"(b.z), "r"(b.w)
+                 : "memory");
+}
 // ... and to a row: a warp's lanes side by side, lane l from column c = c(0) + 8 l on; all 32 take part, those from column `cols` on store nothing.
 // Rows that begin between two words: every lane stores its neighbour's last value with its own first ones, as whole words (byte by byte
 // at the ends, 14336 x 4095 out of 4 bits took 79 us).

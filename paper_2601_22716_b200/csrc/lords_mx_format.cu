@@ -165,27 +165,46 @@ __device__ __forceinline__ uint4 values4(uint32_t w, uint32_t byte)
     return make_uint4(__byte_perm(v[0], v[1], 0x5410), __byte_perm(v[2], v[3], 0x5410), __byte_perm(v[0], v[1], 0x7632), __byte_perm(v[2], v[3], 0x7632));
 }
 
-// A CTA takes 32 rows x 256 columns, a warp four rows, a thread eight values of each.  (128 rows, four after four: 2048 x 4096 9.2 us, 14336 x 4096 28.)
-constexpr int kDThreads = 256, kDRows = 4;
-__global__ void __launch_bounds__(kDThreads) lords_mxfp4_dequantize_kernel(const uint8_t *codes, const uint8_t *scales, int rows,
-                                                                           int cols, int pitch, int ktiles, uint16_t *v)
+// A warp takes four rows x 256 columns, a thread eight values of each (128 rows a CTA, four after four: 2048 x 4096 9.2 us, 14336 x 4096 28, so 4.5 and 24.9);
+// WIDE, rows that begin at 32-byte boundaries: two rows x 512 columns, sixteen values of each.
+constexpr int kDThreads = 256;
+template <bool WIDE>
+__global__ void __launch_bounds__(kDThreads) lords_mxfp4_dequantize_kernel(const uint8_t *codes, const uint8_t *scales, int rows, int cols, int pitch, int ktiles,
+                                                                           uint16_t *v)
 {
+    constexpr int ROWS = WIDE ? 2 : 4, PER = WIDE ? 16 : 8;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int c = (int)blockIdx.x * 256 + lane * 8, r0 = ((int)blockIdx.y * (kDThreads / 32) + warp) * kDRows, b = c / kBlock;
+    const int c = ((int)blockIdx.x * 32 + lane) * PER, r0 = ((int)blockIdx.y * (kDThreads / 32) + warp) * ROWS, b = c / kBlock;
     ptx::griddep_launch_dependents();
     ptx::griddep_wait();
-    // (the four rows lie in one row of tiles)
+    // (the rows lie in one row of tiles)
     const uint8_t *sc = scales + ((size_t)(r0 / kTileRows) * ktiles + b / kTileBlocks) * kTileBytes;
-    uint32_t w[kDRows], e[kDRows];
+    const uint8_t *src = codes + (size_t)r0 * pitch + c / 2;
+    uint32_t w[ROWS][PER / 8], e[ROWS];
 #pragma unroll
-    for (int k = 0; k < kDRows; ++k) {
-        const bool in = r0 + k < rows && c < cols;
-        w[k] = in ? *reinterpret_cast<const uint32_t *>(codes + (size_t)(r0 + k) * pitch + c / 2) : 0u;
-        e[k] = in ? sc[scale_at((r0 + k) % kTileRows, b % kTileBlocks)] : 0u;
+    for (int k = 0; k < ROWS; ++k, src += pitch) {
+        e[k] = 0u;
+#pragma unroll
+        for (int h = 0; h < PER / 8; ++h) w[k][h] = 0u;
+        if (r0 + k >= rows || c >= cols) continue;
+        if constexpr (WIDE) {
+            const uint2 two = *reinterpret_cast<const uint2 *>(src);
+            w[k][0] = two.x; w[k][1] = two.y;
+        } else {
+            w[k][0] = *reinterpret_cast<const uint32_t *>(src);
+        }
+        e[k] = sc[scale_at((r0 + k) % kTileRows, b % kTileBlocks)];
     }
+    uint16_t *row = v + (size_t)r0 * cols;
 #pragma unroll
-    for (int k = 0; k < kDRows; ++k)
-        if (r0 + k < rows) store8(v + (size_t)(r0 + k) * cols, cols, c, values4(w[k], e[k]), lane);
+    for (int k = 0; k < ROWS; ++k, row += cols) {
+        if (r0 + k >= rows) break;
+        if constexpr (WIDE) {
+            if (c < cols) store16(row + c, values4(w[k][0], e[k]), values4(w[k][1], e[k]));
+        } else {
+            store8(row, cols, c, values4(w[k][0], e[k]), lane);
+        }
+    }
 }
 
 }  // namespace
@@ -208,9 +227,13 @@ int launch_mxfp4_quantize(const uint16_t *v, int rows, int cols, uint8_t *codes,
 
 int launch_mxfp4_dequantize(const uint8_t *codes, const uint8_t *scales, int rows, int cols, uint16_t *v, cudaStream_t stream)
 {
-    constexpr int per = kDThreads / 32 * kDRows;
-    const dim3 grid((unsigned)((cols + 255) / 256), (unsigned)((rows + per - 1) / per));
-    return launch_dependent(lords_mxfp4_dequantize_kernel, grid, kDThreads, stream, codes, scales, rows, cols, (int)codes_pitch(cols), scale_tiles_of(cols), v);
+    const int pitch = (int)codes_pitch(cols), ktiles = scale_tiles_of(cols);
+    if (cols % 16 == 0 && reinterpret_cast<uintptr_t>(v) % 32 == 0) {
+        const dim3 grid((unsigned)((cols + 511) / 512), (unsigned)((rows + 15) / 16));
+        return launch_dependent(lords_mxfp4_dequantize_kernel<true>, grid, kDThreads, stream, codes, scales, rows, cols, pitch, ktiles, v);
+    }
+    const dim3 grid((unsigned)((cols + 255) / 256), (unsigned)((rows + 31) / 32));
+    return launch_dependent(lords_mxfp4_dequantize_kernel<false>, grid, kDThreads, stream, codes, scales, rows, cols, pitch, ktiles, v);
 }
 
 }  // namespace lords
