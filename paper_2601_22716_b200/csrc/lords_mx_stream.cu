@@ -13,9 +13,9 @@
 // do not touch each other.
 //
 // Bound: the stream of codes and scales, 17/32 bytes a weight, behind some 2.4 us of launch, set-up and epilogue: 14336 x 4096, one token, codes given
-// 8.3 us, of which the loads alone 7.5 (31 MB in 5.1 us, 6.1 TB/s) and the copies of the scales 0.4; with x in bf16 9.4.  4096 x 4096: 4.0 and
-// 4.6.  Everything is read in the stream's order.  (Asking L2 for the first tiles of W ahead of the previous launch's end:
-// 8.3 -> 8.0 us, but 4.0 -> 4.15 for the smaller layer and 9.8 with all tiles; CTAs small enough for two on an SM 9.0.)
+// 8.0 us, of which the loads alone 7.5 (31 MB in 5.1 us, 6.1 TB/s); with x in bf16 9.0.  4096 x 4096: 3.7 and 4.4.  Everything is read in the
+// stream's order.  (Asking L2 for the first tiles of W ahead of the previous launch's end: 8.3 -> 8.0 us, but 4.0 -> 4.15 for the smaller layer and
+// 9.8 with all tiles; CTAs small enough for two on an SM 9.0: both against the kernel before its last steps.)
 //
 // Every wait is bounded; on expiry the role records LORDS_ERR_TIMEOUT and leaves its loop.
 #include <cuda.h>
@@ -39,6 +39,7 @@ constexpr int kConvWarp0 = 4;                // warps from 4 on: x to 4 bits, th
 constexpr int kSplitMax = 8;                 // CTAs that share a tile's steps
 constexpr int kBatch = 8;                    // x in bf16: steps whose slice of x is converted together
 constexpr int kBatches = 2;                  // ... and batches in shared memory
+constexpr int kStagesMax = 12;
 
 // QX: warps that bring x to 4 bits; 0: x arrives as codes.
 template <int BN, int QX> struct SCfg {
@@ -51,15 +52,21 @@ template <int BN, int QX> struct SCfg {
     static constexpr int XSTEP = XTILE + SF;                        // x of a step with its scales
     static constexpr int STAGE = WTILE + SF + (QX ? 0 : XSTEP);
     static constexpr int XRING = QX ? kBatches * kBatch * XSTEP : 0;
-    // partial sums from the cluster: ceil(groups / split) * split <= groups + split - 1 places of four tokens x 128 rows
-    static constexpr int RECV = (BN / 4 + kSplitMax - 1) * 4 * kRows * 4;
-    static constexpr int ROOM = 232448 - 1024 - 512 - RECV - XRING;
-    static constexpr int STAGES = ROOM / STAGE < 10 ? ROOM / STAGE : 10;
-    static constexpr int SMEM = 1024 + STAGES * STAGE + XRING + RECV + 512;
+    static constexpr int BARS = 16 * kStagesMax + 16 + 16 * kBatches + 8;
+    static constexpr int FIXED = 1024 + XRING + (BARS + 255) / 256 * 256;      // shared memory apart from stages and partial sums
+    static constexpr int SMEM = 232448;
     static constexpr uint32_t ACC = BN < 32 ? 32 : BN;              // accumulator columns; behind them two sets of scales
     static constexpr uint32_t TMEM = ACC + 32 <= 64 ? 64 : ACC + 32 <= 128 ? 128 : 256;
-    static_assert(SMEM <= 232448 && STAGE % 1024 == 0 && XSTEP % 1024 == 0 && STAGES >= 3, "shared memory");
+    static_assert(STAGE % 1024 == 0 && XSTEP % 1024 == 0, "tiles begin at 1024 bytes");
 };
+
+// Tokens that are added up together, and the shared memory of a cluster's partial sums: ceil(groups / split) * split places of a group x 128 rows.
+__host__ __device__ constexpr int group_of(int tokens) { return tokens > 2 ? 4 : tokens; }
+__host__ __device__ constexpr int sums_bytes(int tokens, int split)
+{
+    const int gw = group_of(tokens), groups = (tokens + gw - 1) / gw;
+    return split > 1 ? (groups + split - 1) / split * split * kRows * 4 * gw : 0;
+}
 
 struct alignas(64) StreamParams {
     CUtensorMap tm_w;        // bytes [m][pitch], box {128, 128}, 128-byte swizzle (zeros behind the last row and byte)
@@ -69,6 +76,7 @@ struct alignas(64) StreamParams {
     const uint16_t *x;       // bf16 [M][n]; QX only
     int M, m, n;
     int steps, blocks, ktiles;       // of a row: steps of 256 columns, blocks, scale tiles
+    int stages;              // of the ring: what the partial sums leave room for, and no more than a CTA has steps
     void *y;
     int y_f32;
     int *status;
@@ -141,25 +149,24 @@ template <int BN, int QX>
 __global__ void __launch_bounds__(SCfg<BN, QX>::THREADS, 1) lords_mxfp4_stream_kernel(const __grid_constant__ StreamParams p)
 {
     using C = SCfg<BN, QX>;
-    constexpr int STAGES = C::STAGES;
+    const int stages = p.stages;
     extern __shared__ uint8_t s_smem[];
     const uint32_t base = (smem_u32(s_smem) + 1023u) & ~1023u;
-    const uint32_t xring = base + STAGES * C::STAGE, recv = xring + C::XRING, bars = recv + C::RECV;
-    const uint32_t bar_full = bars, bar_empty = bar_full + 8 * STAGES, bar_acc = bar_empty + 8 * STAGES, bar_recv = bar_acc + 8;
+    const uint32_t xring = base + (uint32_t)(stages * C::STAGE), bars = xring + C::XRING, recv = bars + (C::BARS + 255) / 256 * 256;
+    const uint32_t bar_full = bars, bar_empty = bar_full + 8 * kStagesMax, bar_acc = bar_empty + 8 * kStagesMax, bar_recv = bar_acc + 8;
     const uint32_t bar_x = bar_recv + 8, bar_x_free = bar_x + 8 * kBatches, tmem_slot = bar_x_free + 8 * kBatches;
-    static_assert(16 * STAGES + 16 + 16 * kBatches + 8 <= 512, "barrier area");
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int rank = (int)cluster_ctarank(), split = (int)cluster_nctarank();
     const int rt = (int)(blockIdx.x / split), row0 = rt * kRows, tok0 = (int)blockIdx.y * BN;
     const int s_a = (int)((long long)p.steps * rank / split), s_b = (int)((long long)p.steps * (rank + 1) / split);
     const int tokens = p.M - tok0 < BN ? p.M - tok0 : BN;
-    const int gw = tokens > 2 ? 4 : tokens;               // tokens that are added up together
+    const int gw = group_of(tokens);
     const int *status = p.status;
     bool failed = false;
 
     if (warp == 0) {
         if (lane == 0) {
-            for (int s = 0; s < STAGES; ++s) { mbar_init(bar_full + 8 * s, 1); mbar_init(bar_empty + 8 * s, 1); }
+            for (int s = 0; s < stages; ++s) { mbar_init(bar_full + 8 * s, 1); mbar_init(bar_empty + 8 * s, 1); }
             mbar_init(bar_acc, 1);
             mbar_init(bar_recv, 1);
             for (int s = 0; s < kBatches; ++s) { mbar_init(bar_x + 8 * s, C::CONV); mbar_init(bar_x_free + 8 * s, 1); }
@@ -184,12 +191,13 @@ __global__ void __launch_bounds__(SCfg<BN, QX>::THREADS, 1) lords_mxfp4_stream_k
 
     if (warp == 0) {
         // ------------------------------------------------------------------ TMA: codes and scales of W, and of x.  (Under lane == 0; under elect.sync, which
-        // the kernel on pairs gains by, 14336 x 4096 took 8.3 us in place of 8.0.)
+        // the kernel on pairs gains by, 14336 x 4096 with the codes given took 8.3 us in place of 8.0.)
         if (lane == 0) {
-            int it = 0;
-            for (int st = s_a; st < s_b; ++st, ++it) {
-                const int s = it % STAGES;
-                if (it >= STAGES && !mbar_wait(bar_empty + 8 * s, (uint32_t)((it / STAGES - 1) & 1), status, 61)) { failed = true; break; }
+            int s = 0;
+            uint32_t phase = 1;                // of the empties: the first time around nothing is waited for
+            for (int st = s_a; st < s_b; ++st, s = s + 1 == stages ? 0 : s + 1) {
+                if (s == 0) phase ^= 1u;
+                if (st - s_a >= stages && !mbar_wait(bar_empty + 8 * s, phase ^ 1u, status, 61)) { failed = true; break; }
                 const uint32_t dst = base + (uint32_t)(s * C::STAGE), bar = bar_full + 8 * s;
                 const int kt = p.ktiles - 2 * st < 2 ? 1 : 2;
                 mbar_expect_tx(bar, (uint32_t)(C::WTILE + kt * kTileBytes + (QX ? 0 : C::XTILE + kt * kTileBytes)));
@@ -206,11 +214,13 @@ __global__ void __launch_bounds__(SCfg<BN, QX>::THREADS, 1) lords_mxfp4_stream_k
         // ------------------------------------------------------------------ MMA issuer
         const uint32_t hi = (uint32_t)(umma_desc_sw128(0, 1024, 16) >> 32), lo0 = (uint32_t)umma_desc_sw128(0, 1024, 16);
         const uint32_t tmem_u = warp_uniform(tmem_base), leader = elect_one();
-        int it = 0;
-        for (int st = s_a; st < s_b; ++st, ++it) {
-            const int s = it % STAGES, batch = it / kBatch;
+        int it = 0, s = 0;
+        uint32_t phase = 1;
+        for (int st = s_a; st < s_b; ++st, ++it, s = s + 1 == stages ? 0 : s + 1) {
+            if (s == 0) phase ^= 1u;
+            const int batch = it / kBatch;
             if (QX && it % kBatch == 0 && !mbar_wait_warp(bar_x + 8 * (batch % kBatches), (uint32_t)((batch / kBatches) & 1), status, 66)) { failed = true; break; }
-            if (!mbar_wait_warp(bar_full + 8 * s, (uint32_t)((it / STAGES) & 1), status, 62)) { failed = true; break; }
+            if (!mbar_wait_warp(bar_full + 8 * s, phase, status, 62)) { failed = true; break; }
             tc_fence_after_sync();
             const uint32_t at = base + (uint32_t)(s * C::STAGE), sw = at + C::WTILE;
             const uint32_t xt = QX ? xring + (uint32_t)(it % (kBatch * kBatches) * C::XSTEP) : sw + C::SF, sx = xt + C::XTILE;
@@ -256,7 +266,8 @@ __global__ void __launch_bounds__(SCfg<BN, QX>::THREADS, 1) lords_mxfp4_stream_k
                     }
                 }
             };
-            // A batch is at most WORK tokens x steps of eight blocks, two blocks a thread: block e is block e % (8 count) of token e / (8 count).  The next batch's
+            // A batch is at most WORK tokens x steps of eight blocks, two blocks a thread (a quarter of a block: one token 5.8 us at 4096 x 4096 and 9.1 at
+            // 14336 x 4096, 4.5 and 8.9 so): block e is block e % (8 count) of token e / (8 count).  The next batch's
             // loads are on their way while this one is converted.
             constexpr int PER = C::WORK * 8 / (C::CONV * 32);
             const int steps = s_b - s_a, id = tid - kConvWarp0 * 32;
@@ -409,10 +420,16 @@ template <int BN, int QX> struct StreamVariant {
         if (split < 1) return LORDS_ERR_UNSUPPORTED;
         if (tok_tiles > 65535) return LORDS_ERR_SHAPE;
         const int own = (k.steps + split - 1) / split;
+        const int sums = sums_bytes(k.M < BN ? k.M : BN, split), room = (C::SMEM - C::FIXED - sums) / C::STAGE;
+        k.stages = room < own ? room : own;
+        // (with x in bf16, more loads of W in flight hold up those of x: 14336 x 4096, one token 9.1 us with five to seven stages, 9.7 with twelve, 9.5 with four)
+        constexpr int most = QX > 0 ? 6 : kStagesMax;
+        if (k.stages > most) k.stages = most;
         if (QX > 0 && k.M * (QX == 4 && own > kBatch ? kBatch : own) > C::WORK) return LORDS_ERR_UNSUPPORTED;
         cudaLaunchConfig_t cfg;
         cudaLaunchAttribute attr[2];
         fill(cfg, attr, row_tiles, tok_tiles, split, stream);
+        cfg.dynamicSmemBytes = (size_t)(C::FIXED + sums + k.stages * C::STAGE);
         LORDS_CUDA_TRY(allow(st));
         LORDS_CUDA_TRY(cudaLaunchKernelEx(&cfg, lords_mxfp4_stream_kernel<BN, QX>, k));
         return LORDS_OK;
@@ -463,7 +480,7 @@ int launch_mxfp4_stream(const MxProblem &p, State &st, cudaStream_t stream)
     int rc;
     // x in bf16: up to four tokens four converter warps.  Up to sixteen eight warps, where a CTA has few steps (64 tokens x steps): every row tile converts
     // x again and reads it in 16 bits.  In device time a launch of its own for that is the faster by then (4096 x 4096, 16 tokens of
-    // four steps: 6.2 us here, 5.6 with two launches; 14336 x 4096, sixteen steps: 13.8 and 10.0), but a call from the host takes
+    // four steps: 6.0 us here, 5.6 with two launches; 14336 x 4096, sixteen steps: 13.8 and 9.8), but a call from the host takes
     // 2 us more for two launches (6.0 and 8.1).
     if (qx && p.M <= 4) rc = StreamVariant<16, 4>::launch(k, st, stream);
     else if (qx) rc = StreamVariant<16, 8>::launch(k, st, stream);
