@@ -9,6 +9,7 @@
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
+#include <climits>
 #include <cstring>
 #include <initializer_list>
 
@@ -61,9 +62,11 @@ bool gather(const char *fn, const char *const *names, int count, int required, P
 
 bool to_int(PyObject *o, int *v)
 {
-    const long l = PyLong_AsLong(o);
+    int overflow = 0;
+    const long l = PyLong_AsLongAndOverflow(o, &overflow);
     if (l == -1 && PyErr_Occurred()) return false;
-    *v = (int)l;
+    // what no int holds is out of every range as well: the call refuses it
+    *v = overflow > 0 || l > INT_MAX ? INT_MAX : overflow < 0 || l < INT_MIN ? INT_MIN : (int)l;
     return true;
 }
 

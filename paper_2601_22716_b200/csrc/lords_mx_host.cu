@@ -55,17 +55,36 @@ static int forward_common(const void *x, const uint8_t *w, const uint8_t *ws, in
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     st.last_launches = 0;
     MxProblem p = {static_cast<const uint16_t *>(x), nullptr, nullptr, w, ws, M, m, n, y, y_f32};
-    rc = launch_mxfp4_stream(p, st, s);             // a handful of tokens: one launch
-    if (rc != LORDS_ERR_UNSUPPORTED) return rc;
-    // x in 4 bits lies in the workspace between the two launches
-    const size_t cb = (codes_bytes(M, n) + 255) & ~(size_t)255;
-    if (cb + scales_bytes(M, n) > st.workspace_bytes) return LORDS_ERR_WORKSPACE;
-    uint8_t *xq = st.workspace, *xs = st.workspace + cb;
-    rc = launch_mxfp4_quantize(p.x, M, n, xq, xs, nullptr, nullptr, s);
-    if (rc != LORDS_OK) return rc;
-    st.last_launches = 1;
-    p.x = nullptr; p.xq = xq; p.xs = xs;
-    return product(p, st, s);
+    if (st.forced_path != 8) {                      // a handful of tokens: one launch
+        rc = launch_mxfp4_stream(p, st, s);
+        if (rc != LORDS_ERR_UNSUPPORTED) return rc;
+    }
+    // x in 4 bits lies in the workspace between the two launches.  More tokens than it holds: one part after the other, all on the kernel that a call of
+    // more than 512 tokens takes.
+    auto room = [&](int tokens) { return ((codes_bytes(tokens, n) + 255) & ~(size_t)255) + scales_bytes(tokens, n); };
+    int part = M;
+    if (room(M) > st.workspace_bytes) {
+        for (part = M <= 512 ? 0 : (M - 1) / mx::kTileRows * mx::kTileRows; part > 0 && room(part) > st.workspace_bytes;) {
+            const int half = part / 2 / mx::kTileRows * mx::kTileRows;
+            part = room(half) > st.workspace_bytes || half == 0 ? half : part - mx::kTileRows;
+        }
+        if (part == 0) return LORDS_ERR_WORKSPACE;
+    }
+    int launches = 0;
+    for (int t = 0; t < M; t += part) {
+        MxProblem now = p;
+        now.M = M - t < part ? M - t : part;
+        uint8_t *xq = st.workspace, *xs = st.workspace + ((codes_bytes(now.M, n) + 255) & ~(size_t)255);
+        rc = launch_mxfp4_quantize(p.x + (size_t)t * n, now.M, n, xq, xs, nullptr, nullptr, s);
+        if (rc != LORDS_OK) return rc;
+        now.x = nullptr; now.xq = xq; now.xs = xs;
+        now.y = static_cast<uint8_t *>(y) + (size_t)t * m * (y_f32 ? 4 : 2);
+        rc = part < M ? launch_mxfp4_pair(now, st, s) : product(now, st, s);
+        if (rc != LORDS_OK) return rc;
+        ++launches;
+    }
+    st.last_launches = 2 * launches;
+    return LORDS_OK;
 }
 
 // A gradient call with the values of a checkpoint as the layer's input: they are written to the end of the workspace, which the gradients' launches see

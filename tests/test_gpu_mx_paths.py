@@ -203,3 +203,82 @@ def test_calls_from_two_threads():
     for t in threads:
         t.join()
     assert not bad
+
+
+def test_a_small_workspace_is_gone_through_in_parts():
+    m, n, M = 384, 2048, 1500
+    x, xq, _ = _operand(M, n, 1)
+    _, wq, _ = _operand(m, n, 2, 0.05)
+    want, want32 = torch.empty(M, m, dtype=torch.bfloat16, device="cuda"), torch.empty(M, m, device="cuda")
+    lords.lords_mxfp4_matmul(*xq, *wq, M, m, n, want)
+    lords.lords_mxfp4_matmul(*xq, *wq, M, m, n, want32, f32=True)
+    torch.cuda.synchronize()
+    lords.lords_shutdown()
+    try:
+        for room in (1 << 20, 300 << 10, 150 << 10):
+            lords.lords_init(0, room)
+            for dtype, ref in ((torch.bfloat16, want), (torch.float32, want32)):
+                y = torch.full((M * m + 64,), -7.0, dtype=dtype, device="cuda")
+                lords.lords_mxfp4_forward(x, *wq, M, m, n, y, f32=dtype == torch.float32)
+                assert torch.equal(y[:M * m].reshape(M, m), ref) and bool((y[M * m:] == -7.0).all())
+            assert lords.lords_poll_status() == 0
+        lords.lords_init(0, 100 << 10)          # 128 tokens take 136 KiB
+        with pytest.raises(lords.LordsError) as e:
+            lords.lords_mxfp4_forward(x, *wq, M, m, n, want)
+        assert e.value.status == -9
+    finally:
+        lords.lords_shutdown()
+        lords.lords_init(0, 0)
+
+
+def _at16(t):
+    """The same values 16 bytes into a buffer that begins at a multiple of 32."""
+    whole = torch.empty(t.numel() * t.element_size() + 48, dtype=torch.uint8, device="cuda")
+    part = whole[16:16 + t.numel() * t.element_size()].view(t.dtype).reshape(t.shape)
+    part.copy_(t)
+    assert part.data_ptr() % 32 == 16
+    return part
+
+
+@pytest.mark.parametrize("M,m,n", [(3, 256, 512), (40, 256, 512), (300, 512, 1024)])
+def test_addresses_at_odd_multiples_of_16(M, m, n):
+    x, xq, _ = _operand(M, n, 1)
+    w, wq, _ = _operand(m, n, 2, 0.05)
+    want = torch.empty(M, m, dtype=torch.bfloat16, device="cuda")
+    lords.lords_mxfp4_matmul(*xq, *wq, M, m, n, want)
+    x16, w16 = _at16(x), _at16(w)
+    qs = [_at16(q) for q in (*_four(m, n), *_four(n, m))]
+    lords.lords_mxfp4_quantize(w16, m, n, *qs)
+    ref = [*_four(m, n), *_four(n, m)]
+    lords.lords_mxfp4_quantize(w, m, n, *ref)
+    assert all(torch.equal(a, b) for a, b in zip(qs, ref))
+    y = _at16(torch.empty_like(want))
+    lords.lords_mxfp4_forward(x16, qs[0], qs[1], M, m, n, y)
+    assert torch.equal(y, want)
+    y.zero_()
+    lords.lords_mxfp4_matmul(*[_at16(q) for q in xq], qs[0], qs[1], M, m, n, y)
+    assert torch.equal(y, want)
+    back, back16 = torch.empty_like(w), _at16(torch.empty_like(w))
+    lords.lords_mxfp4_dequantize(*wq, m, n, back)
+    lords.lords_mxfp4_dequantize(*[_at16(q) for q in wq], m, n, back16)
+    assert torch.equal(back, back16)
+    def kept(v, at):
+        q = at(torch.empty(lords.lords_checkpoint_bytes(M, n), dtype=torch.uint8, device="cuda"))
+        e = at(torch.empty(lords.lords_checkpoint_scales_bytes(M, n), dtype=torch.uint8, device="cuda"))
+        out = at(torch.empty_like(v))
+        lords.lords_checkpoint_store(v, M, n, q, e)
+        lords.lords_checkpoint_load(q, e, M, n, out)
+        return q, e, out
+    assert all(torch.equal(a, b) for a, b in zip(kept(x, lambda t: t), kept(x16, _at16)))
+
+
+def test_sizes_that_no_int_holds_are_refused():
+    x, xq, _ = _operand(4, 64, 1)
+    y = torch.empty(4, 4, dtype=torch.bfloat16, device="cuda")
+    for bad in (2**32 + 4, 2**70, -2**40):
+        with pytest.raises(lords.LordsError) as e:
+            lords.lords_mxfp4_matmul(*xq, *xq, bad, 4, 64, y)
+        assert e.value.status == -2
+        with pytest.raises(lords.LordsError) as e:
+            lords.lords_mxfp4_quantize(x, 4, bad, *xq)
+        assert e.value.status == -2
