@@ -37,52 +37,53 @@ struct QuantizeParams {
 
 template <bool ALONG, bool ACROSS> __global__ void __launch_bounds__(kQThreads) lords_mxfp4_quantize_kernel(const QuantizeParams p)
 {
-    constexpr int PER = kQRows / 32;          // rows a thread loads sixteen values of
+    static_assert(kQRows * 4 == kQThreads, "a block of a row to a thread");
     __shared__ __align__(16) uint8_t tile[ACROSS ? kQRows / 32 * kQBlock : 16];
     __shared__ __align__(16) uint8_t sc[kQRows * 4], sct[128 * (kQRows / 32)];
     const int tid = threadIdx.x, r0 = (int)blockIdx.y * kQRows, c0 = (int)blockIdx.x * 128;
-    const int seg = tid & 7, row_in = tid >> 3, c = c0 + seg * 16;
+    const int seg = tid & 3, rl = tid >> 2, c = c0 + seg * kBlock, i = r0 + rl;
     ptx::griddep_launch_dependents();
     ptx::griddep_wait();
-    uint32_t w[PER][8];
-    const uint16_t *src = p.v + (size_t)(r0 + row_in) * p.cols + c;
+    uint32_t w[16];
 #pragma unroll
-    for (int k = 0; k < PER; ++k, src += (size_t)32 * p.cols) {
-        const int i = r0 + k * 32 + row_in;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) w[k][e] = 0u;
-        if (i >= p.rows) continue;
+    for (int e = 0; e < 16; ++e) w[e] = 0u;
+    if (i < p.rows && c < p.cols) {
+        const uint16_t *row = p.v + (size_t)i * p.cols;
         if (p.wide) {
-            if (c < p.cols)
-                asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-                             : "=r"(w[k][0]), "=r"(w[k][1]), "=r"(w[k][2]), "=r"(w[k][3]), "=r"(w[k][4]), "=r"(w[k][5]), "=r"(w[k][6]), "=r"(w[k][7])
-                             : "l"(src));
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                if (h == 0 || c + 16 < p.cols)
+                    asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                                 : "=r"(w[8 * h]), "=r"(w[8 * h + 1]), "=r"(w[8 * h + 2]), "=r"(w[8 * h + 3]), "=r"(w[8 * h + 4]), "=r"(w[8 * h + 5]), "=r"(w[8 * h + 6]),
+                                   "=r"(w[8 * h + 7])
+                                 : "l"(row + c + 16 * h));
         } else {
             const uint16_t *end = p.v + (size_t)p.rows * p.cols;
-            if (c < p.cols) load8(src - c, p.cols, c, end, w[k]);
-            if (c + 8 < p.cols) load8(src - c, p.cols, c + 8, end, w[k] + 4);
+#pragma unroll
+            for (int h = 0; h < 4; ++h)
+                if (c + 8 * h < p.cols) load8(row, p.cols, c + 8 * h, end, w + 4 * h);
         }
     }
-    uint8_t *out_at = p.codes + (size_t)(r0 + row_in) * p.pitch + c / 2;
+    if constexpr (ACROSS) {
+        // (the second half of a row's threads begin with their second 32 bytes: no two of eight neighbours meet in a bank)
+        const bool second = (seg & 2) != 0;
+        uint4 *at = reinterpret_cast<uint4 *>(tile + (rl >> 5) * kQBlock + (rl & 31) * kQPitch + seg * 64);
 #pragma unroll
-    for (int k = 0; k < PER; ++k) {
-        const int rl = k * 32 + row_in;
-        if constexpr (ACROSS) {
-            uint4 *at = reinterpret_cast<uint4 *>(tile + k * kQBlock + row_in * kQPitch + seg * 32);
-            at[0] = make_uint4(w[k][0], w[k][1], w[k][2], w[k][3]);
-            at[1] = make_uint4(w[k][4], w[k][5], w[k][6], w[k][7]);
+        for (int h = 0; h < 4; ++h) {
+            const int g = h ^ 2;
+            at[second ? g : h] = second ? make_uint4(w[4 * g], w[4 * g + 1], w[4 * g + 2], w[4 * g + 3]) : make_uint4(w[4 * h], w[4 * h + 1], w[4 * h + 2], w[4 * h + 3]);
         }
-        if constexpr (ALONG) {
-            uint32_t top = larger(magnitudes(w[k][0]), magnitudes(w[k][1]), magnitudes(w[k][2]));
-            top = larger(top, magnitudes(w[k][3]), magnitudes(w[k][4]));
-            top = larger(top, magnitudes(w[k][5]), magnitudes(w[k][6]));
-            top = larger(top, magnitudes(w[k][7]));
-            top = larger(top, __shfl_xor_sync(0xffffffffu, top, 1));
-            const uint32_t byte = scale_byte<2>(larger_half(top));
-            if (r0 + rl < p.rows && c < p.pitch * 2)
-                *reinterpret_cast<uint2 *>(out_at + (size_t)(k * 32) * p.pitch) = make_uint2(to_codes4(w[k], byte), to_codes4(w[k] + 4, byte));
-            if ((seg & 1) == 0) sc[rl * 4 + (seg >> 1)] = (uint8_t)byte;
-        }
+    }
+    if constexpr (ALONG) {
+        uint32_t top = magnitudes(w[0]);
+#pragma unroll
+        for (int e = 1; e < 15; e += 2) top = larger(top, magnitudes(w[e]), magnitudes(w[e + 1]));
+        top = larger(top, magnitudes(w[15]));
+        const uint32_t byte = scale_byte<2>(larger_half(top));
+        if (i < p.rows && c < p.cols)
+            *reinterpret_cast<uint4 *>(p.codes + (size_t)i * p.pitch + c / 2) =
+                make_uint4(to_codes4(w, byte), to_codes4(w + 4, byte), to_codes4(w + 8, byte), to_codes4(w + 12, byte));
+        sc[rl * 4 + seg] = (uint8_t)byte;
     }
     __syncthreads();
     // a row's four scales are a word of the tile of scales; the rows behind the last are part of it
