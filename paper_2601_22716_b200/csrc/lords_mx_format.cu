@@ -14,13 +14,14 @@ namespace {
 using namespace mx;
 
 // ------------------------------------------------------------------------------------------------ to 4 bits
-// A CTA takes 64 rows x 128 columns.  Along the rows, two neighbouring threads hold a block in registers, sixteen values each.  Along the columns, a
-// thread reads two columns x 32 rows back from shared memory.  Scales meet in shared memory as words of four blocks.
+// A CTA takes 64 rows x 128 columns.  Along the rows, a thread holds a block in registers.  Along the columns, a thread reads two columns x 32 rows back
+// from shared memory.  Scales meet in shared memory as words of four blocks.
 //
-// 14336 x 4096: rows 23.3 us (6.4 TB/s, the copy rate; 30.7 with four threads to a block and 12.6 instructions a value, which kept the issue slots 81 %
-// busy), columns 30.6, both 36 (46.5 with 16-byte stores along the columns; 5.0 TB/s: issue slots 63 % busy, the load/store unit with
-// the tile's way through shared memory).
-constexpr int kQRows = 64;                  // rows per CTA (128: 4 to 8 % slower along the rows and level otherwise; 32: 2 to 10 % slower)
+// 14336 x 4096: rows 22.9 us (6.5 TB/s, the copy rate; with four threads to a block 30.7: 12.6 instructions a value kept the issue slots 81 % busy; with
+// two 24.3), columns 29.8 and both 35.6 (46.5 with 16-byte stores along the columns; 5.0 TB/s: issue slots 67 % busy, load/store unit 61 %).
+// Level or slower: 128 rows a CTA, 32 rows, 256 columns where all eight warps have columns (2048 x 4096 both ways 9.8 us in place of 7.2); rows off 16-byte
+// pitches through shared memory, whole words of a row by neighbouring lanes (14336 x 4095 51 us, 43 so).
+constexpr int kQRows = 64;                  // rows per CTA
 constexpr int kQThreads = 256;
 constexpr int kQPitch = 128 * 2 + 16;       // bytes per row of the tile in shared memory; 16-byte words stay aligned
 constexpr int kQBlock = 32 * kQPitch + 64;  // ... and per 32 rows: the same columns of two neighbouring blocks lie in different banks
