@@ -13,7 +13,8 @@ BLOCK = 32
 
 def bf16_values(bits: np.ndarray) -> np.ndarray:
     """uint16 bf16 bit patterns -> float64."""
-    return (bits.astype(np.uint32) << 16).view(np.float32).astype(np.float64)
+    with np.errstate(invalid="ignore"):         # signalling NaNs
+        return (bits.astype(np.uint32) << 16).view(np.float32).astype(np.float64)
 
 
 def exponents(v: np.ndarray, below: int):

@@ -393,3 +393,127 @@ def test_the_library_s_own_refusals():
     finally:
         lords.lords_shutdown()
         lords.lords_init(0, 0)
+
+
+@pytest.mark.parametrize("order", ["ascending", "shuffled", "with one large value"])
+def test_every_bf16_pattern(order):
+    """All 65536 patterns, subnormal numbers, infinities and NaNs among them, to both formats and back."""
+    bits = np.arange(65536, dtype=np.uint16)
+    if order == "shuffled":                     # nearly every block has a value that is not finite: those apart
+        finite = bits[(bits & 0x7F80) != 0x7F80]
+        bits = np.random.default_rng(1).permutation(finite)
+    bits = bits[: len(bits) // 32 * 32].reshape(-1, 32).copy()
+    if order == "with one large value":         # 1.0 first, so that the others are rounded on its grid
+        bits[:, 0] = 0x3F80
+    v = torch.from_numpy(bits.view(np.int16)).view(torch.bfloat16)
+    v64 = mx.bf16_values(bits)
+    rows, cols = bits.shape
+    codes, E = mx.quantize4(v64)
+    tcodes, tE = mx.quantize4(v64.T.copy())
+    got = _quantize(v.cuda(), True, True)
+    for g, w in zip(got, (*mx.pack4(codes, E), *mx.pack4(tcodes, tE))):
+        assert np.array_equal(g.cpu().numpy(), w)
+    out = torch.empty(rows, cols, dtype=torch.bfloat16, device="cuda")
+    lords.lords_mxfp4_dequantize(got[0], got[1], rows, cols, out)
+    assert np.array_equal(out.double().cpu().numpy(), mx.values4(codes, E), equal_nan=True)
+    q, E8 = mx.quantize8(v64)
+    dq, de = (torch.empty(f(rows, cols), dtype=torch.uint8, device="cuda") for f in (lords.lords_checkpoint_bytes, lords.lords_checkpoint_scales_bytes))
+    lords.lords_checkpoint_store(v.cuda(), rows, cols, dq, de)
+    for g, w in zip((dq, de), mx.pack8(q, E8)):
+        assert np.array_equal(g.cpu().numpy(), w)
+    lords.lords_checkpoint_load(dq, de, rows, cols, out)
+    assert np.array_equal(out.double().cpu().numpy(), mx.values8(q, E8), equal_nan=True)
+    # the same values on the way into a product: one row of identity weights after the other picks them out again
+    eye = torch.eye(cols, dtype=torch.bfloat16, device="cuda")
+    wq = _quantize(eye)[:2]
+    x = v[:4].contiguous().cuda()
+    y = torch.empty(4, cols, device="cuda")
+    lords.lords_mxfp4_forward(x, *wq, 4, cols, cols, y, f32=True)
+    want = mx.values4(codes[:4], E[:4])
+    near = want * (np.abs(want) >= 2.0**-126)   # below fp32's normal numbers a sum may become zero
+    got4 = y.double().cpu().numpy()
+    assert np.array_equal(np.isnan(got4), np.isnan(want)) and ((got4 == want) | (got4 == near) | np.isnan(want)).all()
+
+
+def test_with_the_low_rank_scaled_layers_on_one_stream():
+    """A chain of layers of either kind, activations kept on the way and gradients taken, without a wait between."""
+    M, h, r, bits = 24, 512, 8, 4
+    lay, q, B, A = _layer(h, h, r, M, bits, 3)
+    w = (_values(h, h, 4) * 0.02).to(torch.bfloat16).cuda()
+    wq = _quantize(w)[:2]
+    x0, g = _values(M, h, 5).cuda(), _values(M, h, 6).cuda()
+    torch.cuda.synchronize()
+
+    def chain(wait):
+        done = torch.cuda.synchronize if wait else (lambda: None)
+        out = []
+        x = x0
+        for _ in range(4):
+            a = torch.empty(M, h, dtype=torch.bfloat16, device="cuda")
+            lords.lords_linear_forward_bits(x, q, B, A, lay.codebook, bits, M, h, h, r, a)
+            done()
+            cq = torch.empty(lords.lords_checkpoint_bytes(M, h), dtype=torch.uint8, device="cuda")
+            ce = torch.empty(lords.lords_checkpoint_scales_bytes(M, h), dtype=torch.uint8, device="cuda")
+            lords.lords_checkpoint_store(a, M, h, cq, ce)
+            done()
+            b = torch.empty(M, h, dtype=torch.bfloat16, device="cuda")
+            lords.lords_mxfp4_forward(a, *wq, M, h, h, b)
+            done()
+            dB, dA = torch.empty(h, r, device="cuda"), torch.empty(r, h, device="cuda")
+            lords.lords_linear_backward_factors_checkpoint(g, cq, ce, q, B, A, lay.codebook, bits, M, h, h, r, dB, dA)
+            done()
+            x = b
+            out += [a, b, dB, dA]
+        torch.cuda.synchronize()
+        return out
+
+    want = chain(True)
+    for _ in range(3):
+        assert all(torch.equal(a, b) for a, b in zip(chain(False), want))
+    assert lords.lords_poll_status() == 0
+
+
+def test_a_status_that_a_kernel_left_is_reported_and_cleared():
+    M, m, n = 20, 256, 512
+    x, w = _values(M, n, 1).cuda(), _values(m, n, 2).cuda()
+    wq = _quantize(w)[:2]
+    y = torch.empty(M, m, device="cuda")
+    lords.lords_mxfp4_forward(x, *wq, M, m, n, y, f32=True)
+    want = y.clone()
+    assert lords.lords_poll_status() == 0
+    lords.lords_set_option("inject_status", "-8")
+    for rows in (2, 20):
+        lords.lords_mxfp4_forward(x, *wq, rows, m, n, y)
+    assert lords.lords_poll_status() == -8
+    lords.lords_mxfp4_forward(x, *wq, M, m, n, y, f32=True)
+    assert lords.lords_poll_status() == 0 and torch.equal(y, want)
+
+
+def test_the_first_call_of_a_process_may_be_captured():
+    """Nothing that a capture forbids happens at a kernel's first call."""
+    import subprocess
+    import sys
+    code = """
+import torch
+from paper_2601_22716_b200 import binding as lords
+lords.lords_init(0, 0)
+def four(rows, cols):
+    return [torch.empty(f(rows, cols), dtype=torch.uint8, device="cuda") for f in (lords.lords_mxfp4_codes_bytes, lords.lords_mxfp4_scales_bytes)]
+m, n = 512, 1024
+w = torch.randn(m, n, device="cuda").to(torch.bfloat16)
+for M in (1, 12, 48, 100, 700):
+    x, y = torch.randn(M, n, device="cuda").to(torch.bfloat16), torch.zeros(M, m, device="cuda")
+    q, back = four(m, n), torch.zeros_like(w)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        lords.lords_mxfp4_quantize(w, m, n, *q)
+        lords.lords_mxfp4_dequantize(*q, m, n, back)
+        lords.lords_mxfp4_forward(x, *q, M, m, n, y, f32=True)
+    g.replay()
+    torch.cuda.synchronize()
+    z = torch.empty_like(y)
+    lords.lords_mxfp4_forward(x, *q, M, m, n, z, f32=True)
+    assert lords.lords_poll_status() == 0 and torch.equal(y, z) and bool(back.any()) and bool(y.any())
+"""
+    subprocess.run([sys.executable, "-c", code], check=True)
