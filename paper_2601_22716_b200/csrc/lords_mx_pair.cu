@@ -8,7 +8,7 @@
 //
 // Bound: 4-bit MMAs (four times the bf16 rate, 512 cycles a step at BN = 256) and what L2 gives, 128 (128 + BN / 2) bytes of codes a step and CTA: all SMs
 // together read 13 to 14 TB/s with either BN (0.29 and 0.36 us a step), with L2's own units at 36 % and the clock at 1.64 GHz under the
-// power limit.  2048 tokens: 4096 x 14336 44 us (5.5 PFLOP/s), 14336 x 4096 48, its weight gradient 66.  The copies of the
+// power limit.  2048 tokens: 4096 x 14336 44 us (5.5 PFLOP/s), 14336 x 4096 48, its weight gradient in 32 bits 63.  The copies of the
 // scales cost 3 % of that (left out: 42.5); a step's copies ahead of the step before's MMAs, or between them, cost 17 to 30 % more.
 // No scratch memory.  Every wait is bounded; on expiry the role records LORDS_ERR_TIMEOUT and leaves its loop.
 #include <cuda.h>
@@ -55,11 +55,27 @@ struct alignas(64) PairParams {
     CUtensorMap tm_y;        // y, box {128 bytes, 32 rows}, 128-byte swizzle; used if rows of y are 16-byte multiples
     int y_by_tma;
     int M, m;
-    int tok_tiles, tiles, steps, blocks;
+    int tok_tiles, w_tiles, tiles, steps, blocks;
     int pairs;
     void *y;
     int y_f32;
     int *status;
+
+    // Tiles go in bands of eight out-feature tiles, token tile after token tile.  (All token tiles of one out-feature tile first: weight gradients of 4096 x
+    // 14336 and 2048 columns 67.5 us, of 14336 x 4096 and 512 columns 48.8; all out-feature tiles first 62.6 and 41.9, but 14336 x 4096 and 2048
+    // columns 66.9; so 62.1, 45.3 and 63.5.  Results in bf16 are level.)
+    __device__ __forceinline__ void place(int tile, int &wt, int &tt) const
+    {
+        constexpr int kBand = 8;
+        if (tok_tiles == 1) {            // (a division is a tenth of a microsecond of a small call)
+            tt = 0;
+            wt = tile;
+            return;
+        }
+        const int per = tok_tiles * kBand, band = tile < per ? 0 : tile / per, in = tile - band * per, wide = w_tiles - band * kBand;
+        tt = wide >= kBand ? in / kBand : in / wide;
+        wt = band * kBand + in - tt * (wide < kBand ? wide : kBand);
+    }
 };
 
 __device__ __forceinline__ uint32_t pack_bf16(uint32_t lo, uint32_t hi)
@@ -118,7 +134,8 @@ __global__ void __launch_bounds__(PCfg<BN>::THREADS, 1) lords_mxfp4_pair_kernel(
             const uint32_t full0 = map_to_rank(bar_full, 0);
             int it = 0;
             for (int tile = pair; tile < p.tiles && !failed; tile += p.pairs) {
-                const int wt = tile / p.tok_tiles, tt = tile - wt * p.tok_tiles;
+                int wt, tt;
+                p.place(tile, wt, tt);
                 for (int k = 0; k < p.steps; ++k, ++it) {
                     const int s = it % STAGES;
                     if (it >= STAGES && !mbar_wait(bar_empty + 8 * s, (uint32_t)((it / STAGES - 1) & 1), status, 71)) { failed = true; break; }
@@ -181,7 +198,9 @@ __global__ void __launch_bounds__(PCfg<BN>::THREADS, 1) lords_mxfp4_pair_kernel(
         const uint32_t own = out_s + (uint32_t)((warp - kPEpiWarp0) * 4096), row = own + (uint32_t)(lane * 128);
         int n = 0;
         for (int tile = pair; tile < p.tiles; tile += p.pairs, ++n) {
-            const int a = n % C::ACCS, wt = tile / p.tok_tiles, tt = tile - wt * p.tok_tiles;
+            const int a = n % C::ACCS;
+            int wt, tt;
+            p.place(tile, wt, tt);
             if (!__all_sync(0xffffffffu, mbar_wait_cluster(bar_acc_full + 8 * a, (uint32_t)((n / C::ACCS) & 1), status, 75))) { failed = true; break; }
             tc_fence_after_sync();
             const int t0 = tt * kPTokens + rank * 128 + q * 32;
@@ -333,7 +352,8 @@ template <int BN> int run_pair(const MxProblem &p, State &st, cudaStream_t strea
         return LORDS_ERR_CUDA;
     k.M = p.M; k.m = p.m;
     k.tok_tiles = (p.M + kPTokens - 1) / kPTokens;
-    const long long tiles = (long long)k.tok_tiles * ((p.m + BN - 1) / BN);
+    k.w_tiles = (p.m + BN - 1) / BN;
+    const long long tiles = (long long)k.tok_tiles * k.w_tiles;
     if (tiles > 2147483647LL - 65536) return LORDS_ERR_SHAPE;
     k.tiles = (int)tiles;
     k.steps = (p.n + 255) / 256;
