@@ -38,8 +38,7 @@ __global__ void __launch_bounds__(kCThreads) lords_checkpoint_store_kernel(const
                          : "=r"(w[k][0]), "=r"(w[k][1]), "=r"(w[k][2]), "=r"(w[k][3]), "=r"(w[k][4]), "=r"(w[k][5]), "=r"(w[k][6]), "=r"(w[k][7])
                          : "l"(row + c));
         } else {
-            load8(row, n, c, end, w[k]);
-            if (c + 8 < n) load8(row, n, c + 8, end, w[k] + 4);
+            load_values<8>(row, n, c, end, w[k]);
         }
     }
 #pragma unroll

@@ -20,7 +20,7 @@ using namespace mx;
 // 14336 x 4096: rows 22.9 us (6.5 TB/s, the copy rate; with four threads to a block 30.7: 12.6 instructions a value kept the issue slots 81 % busy; with
 // two 24.3), columns 29.8 and both 35.6 (46.5 with 16-byte stores along the columns; 5.0 TB/s: issue slots 67 % busy, load/store unit 61 %).
 // Level or slower: 128 rows a CTA, 32 rows, 256 columns where all eight warps have columns (2048 x 4096 both ways 9.8 us in place of 7.2); rows off 16-byte
-// pitches through shared memory, whole words of a row by neighbouring lanes (14336 x 4095 51 us, 43 so).
+// pitches through shared memory, whole words of a row by neighbouring lanes (14336 x 4095 51 us, 32 so).
 constexpr int kQRows = 64;                  // rows per CTA
 constexpr int kQThreads = 256;
 constexpr int kQPitch = 128 * 2 + 16;       // bytes per row of the tile in shared memory; 16-byte words stay aligned
@@ -59,10 +59,7 @@ template <bool ALONG, bool ACROSS> __global__ void __launch_bounds__(kQThreads) 
                                    "=r"(w[8 * h + 7])
                                  : "l"(row + c + 16 * h));
         } else {
-            const uint16_t *end = p.v + (size_t)p.rows * p.cols;
-#pragma unroll
-            for (int h = 0; h < 4; ++h)
-                if (c + 8 * h < p.cols) load8(row, p.cols, c + 8 * h, end, w + 4 * h);
+            load_values<16>(row, p.cols, c, p.v + (size_t)p.rows * p.cols, w);
         }
     }
     if constexpr (ACROSS) {

@@ -13,7 +13,7 @@
 // do not touch each other.
 //
 // Bound: the stream of codes and scales, 17/32 bytes a weight, behind some 2.4 us of launch, set-up and epilogue: 14336 x 4096, one token, codes given
-// 8.0 us, of which the loads alone 7.5 (31 MB in 5.1 us, 6.1 TB/s); with x in bf16 9.0.  4096 x 4096: 3.7 and 4.4.  Everything is read in the
+// 7.9 us, of which the loads alone 7.5 (31 MB in 5.1 us, 6.1 TB/s); with x in bf16 8.5.  4096 x 4096: 3.7 and 4.4.  Everything is read in the
 // stream's order.  (Asking L2 for the first tiles of W ahead of the previous launch's end: 8.3 -> 8.0 us, but 4.0 -> 4.15 for the smaller layer and
 // 9.8 with all tiles; CTAs small enough for two on an SM 9.0: both against the kernel before its last steps.)
 //
@@ -246,26 +246,6 @@ __global__ void __launch_bounds__(SCfg<BN, QX>::THREADS, 1) lords_mxfp4_stream_k
         if constexpr (QX > 0) {
             // -------------------------------------------------------------- x to 4 bits, a block at a time, a batch of steps after the other.  (Tokens
             // from M on are columns of the product that nobody reads: whatever their shared memory holds.)
-            auto load = [&](int t, int c, uint32_t (&w)[16]) {
-                const uint16_t *src = p.x + (size_t)t * p.n + c;
-#pragma unroll
-                for (int k = 0; k < 16; ++k) w[k] = 0u;
-                if (c >= p.n) return;
-                if ((p.n & 7) == 0) {
-#pragma unroll
-                    for (int k = 0; k < 4; ++k)
-                        if (c + 8 * k < p.n) {
-                            const uint4 v = __ldcg(reinterpret_cast<const uint4 *>(src) + k);
-                            w[4 * k] = v.x; w[4 * k + 1] = v.y; w[4 * k + 2] = v.z; w[4 * k + 3] = v.w;
-                        }
-                } else {
-#pragma unroll
-                    for (int k = 0; k < 16; ++k) {
-                        const uint32_t lo = c + 2 * k < p.n ? __ldcg(src + 2 * k) : 0u, up = c + 2 * k + 1 < p.n ? __ldcg(src + 2 * k + 1) : 0u;
-                        w[k] = lo | up << 16;
-                    }
-                }
-            };
             // A batch is at most WORK tokens x steps of eight blocks, two blocks a thread (a quarter of a block: one token 5.8 us at 4096 x 4096 and 9.1 at
             // 14336 x 4096, 4.5 and 8.9 so): block e is block e % (8 count) of token e / (8 count).  The next batch's
             // loads are on their way while this one is converted.
@@ -281,7 +261,11 @@ __global__ void __launch_bounds__(SCfg<BN, QX>::THREADS, 1) lords_mxfp4_stream_k
 #pragma unroll
                 for (int h = 0; h < PER; ++h) {
                     int t, kb;
-                    if (first < steps && place(first, h, t, kb)) load(t, (s_a + first) * kStep + kb * kBlock, w[h]);
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) w[h][k] = 0u;
+                    if (first >= steps || !place(first, h, t, kb)) continue;
+                    const int c = (s_a + first) * kStep + kb * kBlock;
+                    if (c < p.n) load_values<16>(p.x + (size_t)t * p.n, p.n, c, p.x + (size_t)p.M * p.n, w[h]);
                 }
             };
             uint32_t w[PER][16], next[PER][16];

@@ -99,6 +99,37 @@ def test_a_layer_s_token_counts_agree():
         assert torch.equal(a, b), M
 
 
+@pytest.mark.parametrize("cols", [33, 34, 35, 36, 37, 38, 39, 41, 63, 95, 127, 129, 131, 250, 517, 1023])
+def test_rows_that_begin_anywhere(cols):
+    """Row i of a width of 8 k + d begins d i values behind a 16-byte boundary, and the last one ends inside a word: what is read equals the same
+    rows of a tensor whose width leaves them aligned, the values behind them zero."""
+    wide = (cols + 31) // 32 * 32
+    for rows in (1, 2, 5, 8, 9, 70):
+        gen = torch.Generator(device="cuda").manual_seed(rows * 4096 + cols)
+        v = torch.randn(rows, cols, generator=gen, device="cuda").to(torch.bfloat16)
+        room = torch.full((rows * cols + 16,), float("inf"), dtype=torch.bfloat16, device="cuda")       # what lies behind belongs to nothing
+        room[:rows * cols] = v.reshape(-1)
+        odd, even = room[:rows * cols], torch.zeros(rows, wide, dtype=torch.bfloat16, device="cuda")
+        even[:, :cols] = v
+        a, at, b, bt = _four(rows, cols), _four(cols, rows), _four(rows, wide), _four(wide, rows)
+        lords.lords_mxfp4_quantize(odd, rows, cols, *a, *at)
+        lords.lords_mxfp4_quantize(even, rows, wide, *b, *bt)
+        assert all(torch.equal(x, y) for x, y in zip(a, b)), rows
+        pitch = lords.lords_mxfp4_codes_bytes(1, rows)
+        assert torch.equal(at[0], bt[0][:cols * pitch]), rows
+        size = lords.lords_checkpoint_bytes(rows, cols), lords.lords_checkpoint_scales_bytes(rows, cols)
+        assert size == (lords.lords_checkpoint_bytes(rows, wide), lords.lords_checkpoint_scales_bytes(rows, wide))
+        one, two = ([torch.zeros(k, dtype=torch.uint8, device="cuda") for k in size] for _ in range(2))
+        lords.lords_checkpoint_store(odd, rows, cols, *one)
+        lords.lords_checkpoint_store(even, rows, wide, *two)
+        assert all(torch.equal(x, y) for x, y in zip(one, two)), rows
+        _, wq, _ = _operand(40, cols, 9)
+        y, z = torch.empty(rows, 40, device="cuda"), torch.empty(rows, 40, device="cuda")
+        lords.lords_mxfp4_matmul(*a, *wq, rows, 40, cols, y, f32=True)
+        lords.lords_mxfp4_forward(odd, *wq, rows, 40, cols, z, f32=True)
+        assert torch.equal(y, z), rows
+
+
 def test_sizes_past_32_bits():
     """More than 2^31 values, more than 2^32 bytes: the last rows and columns of every call."""
     rows, cols = 140000, 16000                # 2.24e9 values, 4.5 GB
