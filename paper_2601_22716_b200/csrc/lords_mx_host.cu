@@ -21,14 +21,19 @@ static size_t scales_bytes(int rows, int cols) { return (size_t)((rows + mx::kTi
 
 static bool dims_ok(int64_t rows, int64_t cols) { return rows >= 1 && cols >= 1 && rows <= LORDS_MX_DIM_MAX && cols <= LORDS_MX_DIM_MAX; }
 
-static int product(const MxProblem &p, State &st, cudaStream_t s)
+// Whether a product takes the kernel for few tokens, else the one on pairs.
+static bool few_tokens(const MxProblem &p, const State &st)
 {
-    if (st.forced_path == 2) return launch_mxfp4_stream(p, st, s);
-    if (st.forced_path == 8) return launch_mxfp4_pair(p, st, s);
+    if (st.forced_path == 2) return true;
+    if (st.forced_path == 8) return false;
     // Up to 32 tokens the one was never slower, from 513 on the other; between, by their estimates: 128 tokens, 14336 x 4096 15.7 us and 12.0, 4096 x
     // 4096 9.1 and 9.5; 256 tokens, 4096 x 4096 12.8 and 9.9, 1024 x 4096 7.7 and 8.9.
-    const bool few = p.M <= 32 || (p.M <= 512 && mxfp4_stream_us(p, st) <= mxfp4_pair_us(p, st));
-    return few ? launch_mxfp4_stream(p, st, s) : launch_mxfp4_pair(p, st, s);
+    return p.M <= 32 || (p.M <= 512 && mxfp4_stream_us(p, st) <= mxfp4_pair_us(p, st));
+}
+
+static int product(const MxProblem &p, State &st, cudaStream_t s)
+{
+    return few_tokens(p, st) ? launch_mxfp4_stream(p, st, s) : launch_mxfp4_pair(p, st, s);
 }
 
 static int matmul_common(const uint8_t *xq, const uint8_t *xs, const uint8_t *w, const uint8_t *ws, int M, int m, int n, void *y, int y_f32, void *stream)
@@ -55,13 +60,15 @@ static int forward_common(const void *x, const uint8_t *w, const uint8_t *ws, in
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     st.last_launches = 0;
     MxProblem p = {static_cast<const uint16_t *>(x), nullptr, nullptr, w, ws, M, m, n, y, y_f32};
-    if (st.forced_path != 8) {                      // a handful of tokens: one launch
+    auto room = [&](int tokens) { return ((codes_bytes(tokens, n) + 255) & ~(size_t)255) + scales_bytes(tokens, n); };
+    // One launch, where the kernel takes x in bf16.  (From 17 tokens on only if the workspace would hold x in 4 bits as well: a program that reserves too
+    // little learns it from every layer, not from the ones with many steps alone.)
+    if ((M <= 16 || (M <= 64 && room(M) <= st.workspace_bytes)) && few_tokens(p, st)) {
         rc = launch_mxfp4_stream(p, st, s);
         if (rc != LORDS_ERR_UNSUPPORTED) return rc;
     }
     // x in 4 bits lies in the workspace between the two launches.  More tokens than it holds: one part after the other, all on the kernel that a call of
     // more than 512 tokens takes.
-    auto room = [&](int tokens) { return ((codes_bytes(tokens, n) + 255) & ~(size_t)255) + scales_bytes(tokens, n); };
     int part = M;
     if (room(M) > st.workspace_bytes) {
         for (part = M <= 512 ? 0 : (M - 1) / mx::kTileRows * mx::kTileRows; part > 0 && room(part) > st.workspace_bytes;) {

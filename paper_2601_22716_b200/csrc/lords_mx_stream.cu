@@ -4,8 +4,8 @@
 // CTA streams 128 rows of W through shared memory by TMA, 256 columns a step, as the MMA's 128-row operand; the tokens are its N = BN columns.
 // The scales of a step follow their codes through shared memory and from there into TMEM (tcgen05.cp), where the MMA reads them.
 //
-//   QX:    x arrives in bf16; four or eight warps bring it to 4 bits on the way, eight steps' slices at a time: for calls of a handful of
-//          tokens, or of few steps a CTA.
+//   QX:    x arrives in bf16; warps bring it to 4 bits on the way: four of them, eight steps' slices at a time, for calls of up to four tokens;
+//          sixteen, all at once, for calls of more tokens but few steps a CTA.
 //   QX 0:  x arrives as codes and scales, by TMA like W.
 //
 // A cluster of CTAs divides a tile's steps where the row tiles alone leave SMs idle; tokens are added up four at a time, group g by CTA g mod cluster in
@@ -37,22 +37,24 @@ constexpr int kRows = 128;                   // rows of W per CTA
 constexpr int kStep = 256;                   // columns a step: 128 bytes of codes
 constexpr int kConvWarp0 = 4;                // warps from 4 on: x to 4 bits, then (the first four) the epilogue; 0: TMA, 1: MMA issuer, 2: TMEM
 constexpr int kSplitMax = 8;                 // CTAs that share a tile's steps
-constexpr int kBatch = 8;                    // x in bf16: steps whose slice of x is converted together
-constexpr int kBatches = 2;                  // ... and batches in shared memory
 constexpr int kStagesMax = 12;
 
 // QX: warps that bring x to 4 bits; 0: x arrives as codes.
 template <int BN, int QX> struct SCfg {
     static constexpr int CONV = QX > 4 ? QX : 4;                    // converter and epilogue warps
     static constexpr int THREADS = (kConvWarp0 + CONV) * 32;
-    static constexpr int WORK = QX * 8;                             // most tokens x steps of a batch: two blocks a thread
+    // most tokens x steps of a batch (four warps two blocks a thread, sixteen one); steps whose slice of x is converted together, and such batches in shared
+    // memory; sixteen warps: one, of the steps that the fewest tokens of this tile may have
+    static constexpr int WORK = QX == 16 ? 64 : QX * 8;
+    static constexpr int BATCH = QX == 16 ? WORK / (BN == 16 ? 5 : BN / 2 + 1) : 8;
+    static constexpr int BATCHES = QX == 16 ? 1 : 2;
     static constexpr int WTILE = kRows * 128;
     static constexpr int XTILE = BN * 128;
     static constexpr int SF = 2 * kTileBytes;                       // scales of a step: two tiles of four blocks
     static constexpr int XSTEP = XTILE + SF;                        // x of a step with its scales
     static constexpr int STAGE = WTILE + SF + (QX ? 0 : XSTEP);
-    static constexpr int XRING = QX ? kBatches * kBatch * XSTEP : 0;
-    static constexpr int BARS = 16 * kStagesMax + 16 + 16 * kBatches + 8;
+    static constexpr int XRING = QX ? BATCHES * BATCH * XSTEP : 0;
+    static constexpr int BARS = 16 * kStagesMax + 16 + 16 * BATCHES + 8;
     static constexpr int FIXED = 1024 + XRING + (BARS + 255) / 256 * 256;      // shared memory apart from stages and partial sums
     static constexpr int SMEM = 232448;
     static constexpr uint32_t ACC = BN < 32 ? 32 : BN;              // accumulator columns; behind them two sets of scales
@@ -149,6 +151,7 @@ template <int BN, int QX>
 __global__ void __launch_bounds__(SCfg<BN, QX>::THREADS, 1) lords_mxfp4_stream_kernel(const __grid_constant__ StreamParams p)
 {
     using C = SCfg<BN, QX>;
+    constexpr int kBatch = C::BATCH, kBatches = C::BATCHES;
     const int stages = p.stages;
     extern __shared__ uint8_t s_smem[];
     const uint32_t base = (smem_u32(s_smem) + 1023u) & ~1023u;
@@ -272,7 +275,7 @@ __global__ void __launch_bounds__(SCfg<BN, QX>::THREADS, 1) lords_mxfp4_stream_k
             load_batch(0, w);
             for (int first = 0; first < steps && !failed; first += kBatch) {
                 const int batch = first / kBatch;
-                load_batch(first + kBatch, next);
+                if constexpr (kBatches > 1) load_batch(first + kBatch, next);
                 if (batch >= kBatches && !mbar_wait_warp(bar_x_free + 8 * (batch % kBatches), (uint32_t)((batch / kBatches - 1) & 1), status, 63)) { failed = true; break; }
                 const uint32_t to = xring + (uint32_t)((batch % kBatches) * kBatch * C::XSTEP);
 #pragma unroll
@@ -409,7 +412,7 @@ template <int BN, int QX> struct StreamVariant {
         // (with x in bf16, more loads of W in flight hold up those of x: 14336 x 4096, one token 9.1 us with five to seven stages, 9.7 with twelve, 9.5 with four)
         constexpr int most = QX > 0 ? 6 : kStagesMax;
         if (k.stages > most) k.stages = most;
-        if (QX > 0 && k.M * (QX == 4 && own > kBatch ? kBatch : own) > C::WORK) return LORDS_ERR_UNSUPPORTED;
+        if (QX > 0 && k.M * (QX == 4 && own > C::BATCH ? C::BATCH : own) > C::WORK) return LORDS_ERR_UNSUPPORTED;
         cudaLaunchConfig_t cfg;
         cudaLaunchAttribute attr[2];
         fill(cfg, attr, row_tiles, tok_tiles, split, stream);
@@ -456,18 +459,20 @@ int launch_mxfp4_stream(const MxProblem &p, State &st, cudaStream_t stream)
     k.status = st.status_word;
     const bool qx = p.x != nullptr;
     const int bn = tile_for(p.M);
-    if (qx && bn > 16) return LORDS_ERR_UNSUPPORTED;
+    if (qx && bn > 64) return LORDS_ERR_UNSUPPORTED;
     const uint64_t pitch = (uint64_t)codes_pitch(p.n);
     if (!make_map_2d(&k.tm_w, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, p.w, pitch, (uint64_t)p.m, 128, kRows, CU_TENSOR_MAP_SWIZZLE_128B)) return LORDS_ERR_CUDA;
     if (qx) k.tm_x = k.tm_w;
     else if (!make_map_2d(&k.tm_x, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, p.xq, pitch, (uint64_t)p.M, 128, (uint32_t)bn, CU_TENSOR_MAP_SWIZZLE_128B)) return LORDS_ERR_CUDA;
     int rc;
-    // x in bf16: up to four tokens four converter warps.  Up to sixteen eight warps, where a CTA has few steps (64 tokens x steps): every row tile converts
-    // x again and reads it in 16 bits.  In device time a launch of its own for that is the faster by then (4096 x 4096, 16 tokens of
-    // four steps: 6.0 us here, 5.6 with two launches; 14336 x 4096, sixteen steps: 13.8 and 9.8), but a call from the host takes
-    // 2 us more for two launches (6.0 and 8.1).
+    // x in bf16: up to four tokens four converter warps.  Up to 64 tokens sixteen warps, where a CTA has few steps (64 tokens x steps, a block a thread): every
+    // row tile converts x again and reads it in 16 bits.  4096 x 4096, 16 tokens of four steps: 5.7 us, with eight warps 5.8, with two launches
+    // 5.6; 1024 x 4096, 32 tokens of two steps 4.9, with two launches 5.4.  With twice as many blocks a thread, 4096 x 4096, 32 tokens of
+    // four steps takes 7.5 us, 6.3 with two launches.  A call from the host takes 2 us more for two launches (5.7 and 7.9).
     if (qx && p.M <= 4) rc = StreamVariant<16, 4>::launch(k, st, stream);
-    else if (qx) rc = StreamVariant<16, 8>::launch(k, st, stream);
+    else if (qx && bn == 16) rc = StreamVariant<16, 16>::launch(k, st, stream);
+    else if (qx && bn == 32) rc = StreamVariant<32, 16>::launch(k, st, stream);
+    else if (qx) rc = StreamVariant<64, 16>::launch(k, st, stream);
     else if (bn == 16) rc = StreamVariant<16, 0>::launch(k, st, stream);
     else if (bn == 32) rc = StreamVariant<32, 0>::launch(k, st, stream);
     else if (bn == 64) rc = StreamVariant<64, 0>::launch(k, st, stream);

@@ -99,6 +99,25 @@ def test_a_layer_s_token_counts_agree():
         assert torch.equal(a, b), M
 
 
+@pytest.mark.parametrize("m,n", [(129, 40), (300, 256), (640, 700), (260, 1000), (1000, 2731), (4096, 4096), (5000, 513), (70, 12000), (20000, 256)])
+def test_a_layer_on_one_launch_or_two(m, n):
+    """Few steps a CTA: x is converted inside the product's launch up to 64 tokens x steps, by a launch of its own above; both have the same bits."""
+    wide = (n + 7) // 8 * 8
+    _, wq, _ = _operand(m, n, 3, 0.05)
+    x, _, _ = _operand(72, wide, 4)
+    x = x[:, :n].contiguous()
+    launches = set()
+    for M in (5, 6, 8, 10, 12, 13, 16, 17, 20, 21, 22, 31, 32, 33, 40, 63, 64, 65, 72):
+        xq = _four(M, n)
+        lords.lords_mxfp4_quantize(x, M, n, *xq)
+        a, b = torch.empty(M, m, dtype=torch.bfloat16, device="cuda"), torch.full((M * m + 64,), -7.0, dtype=torch.bfloat16, device="cuda")
+        lords.lords_mxfp4_matmul(*xq, *wq, M, m, n, a)
+        lords.lords_mxfp4_forward(x, *wq, M, m, n, b)
+        launches.add(lords.lords_last_launch_count())
+        assert torch.equal(a, b[:M * m].reshape(M, m)) and bool((b[M * m:] == -7.0).all()), M
+    assert launches <= {1, 2}
+
+
 @pytest.mark.parametrize("cols", [33, 34, 35, 36, 37, 38, 39, 41, 63, 95, 127, 129, 131, 250, 517, 1023])
 def test_rows_that_begin_anywhere(cols):
     """Row i of a width of 8 k + d begins d i values behind a 16-byte boundary, and the last one ends inside a word: what is read equals the same
