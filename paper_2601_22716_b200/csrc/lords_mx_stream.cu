@@ -96,42 +96,69 @@ template <int GW> __device__ __forceinline__ void send(uint32_t addr, const uint
                      "r"(v[3]), "r"(bar) : "memory");
 }
 
-// The cluster's sums: tokens in groups of GW, group g to rank g mod cluster; a received value's place is (group / cluster, rank, row).
-template <int BN, int GW>
-__device__ __forceinline__ bool add_up(const StreamParams &p, uint32_t acc, uint32_t recv, uint32_t bar_recv, int rank, int split, int tokens, int tok0, int ri,
-                                       int i, bool failed)
+__device__ __forceinline__ void put(float *at, float v) { *at = v; }
+__device__ __forceinline__ void put(__nv_bfloat16 *at, float v) { *at = __float2bfloat16_rn(v); }
+
+// The sums of a row (y: where its value of token 0 goes, `inside`: it is a row of W) as the one CTA of a tile has them.
+template <int BN, class T> __device__ __forceinline__ void write_out(uint32_t acc, int tokens, T *y, int m, bool inside)
 {
+    const size_t pitch = (size_t)m;
+#pragma unroll 1
+    for (int c0 = 0; c0 < tokens; c0 += 16, y += 16 * pitch) {
+        uint32_t v[16];
+        tmem_ld_32x16(acc + (uint32_t)c0, v);
+        tmem_wait_ld(v);
+        const int left = inside ? tokens - c0 : 0;
+        T *at = y;
+#pragma unroll
+        for (int c = 0; c < 16; ++c, at += pitch)
+            if (c < left) put(at, __uint_as_float(v[c]));
+    }
+}
+
+// The cluster's sums: tokens in groups of GW, group g to rank g mod cluster; a received value's place is (group / cluster, rank, row).
+template <int BN, int GW, class T>
+__device__ __forceinline__ bool add_up(uint32_t acc, uint32_t recv, uint32_t bar_recv, int rank, int split, int tokens, T *y, int m, bool inside, int ri,
+                                       const int *status, bool failed)
+{
+    constexpr uint32_t PLACE = kRows * 4 * GW;
     const int groups = (tokens + GW - 1) / GW;
     const uint32_t row_at = recv + (uint32_t)(ri * 4 * GW);
-#pragma unroll
-    for (int c0 = 0; c0 < BN; c0 += 16) {
-        if (c0 >= tokens) break;
+    int to = 0;
+    uint32_t where = row_at + (uint32_t)rank * PLACE;
+#pragma unroll 1
+    for (int c0 = 0; c0 < tokens; c0 += 16) {
         uint32_t v[16];
         tmem_ld_32x16(acc + (uint32_t)c0, v);
         tmem_wait_ld(v);
 #pragma unroll
         for (int c = 0; c < 16 && (GW == 4 || c == 0); c += GW) {
-            const int g = (c0 + c) / GW;
-            if (g < groups) {
-                const int to = g % split;
-                const uint32_t where = row_at + (uint32_t)(((g / split) * split + rank) * kRows * 4 * GW);
-                if (to == rank) {
+            if (c0 + c >= tokens) break;
+            if (to == rank) {
+                if constexpr (GW == 4) {
+                    sts_v4(where, make_uint4(v[c], v[c + 1], v[c + 2], v[c + 3]));
+                } else {
 #pragma unroll
                     for (int k = 0; k < GW; ++k) sts_u32(where + 4 * k, v[c + k]);
-                } else {
-                    send<GW>(map_to_rank(where, (uint32_t)to), v + c, map_to_rank(bar_recv, (uint32_t)to));
                 }
+            } else {
+                send<GW>(map_to_rank(where, (uint32_t)to), v + c, map_to_rank(bar_recv, (uint32_t)to));
             }
+            if (++to == split) { to = 0; where += (uint32_t)split * PLACE; }
         }
     }
     if (rank >= groups) return true;
-    if (!__all_sync(0xffffffffu, mbar_wait_cluster(bar_recv, 0, p.status, 65))) return false;
-    for (int g = rank; g < groups && !failed; g += split) {
+    if (!__all_sync(0xffffffffu, mbar_wait_cluster(bar_recv, 0, status, 65))) return false;
+    if (failed) return true;
+    const size_t pitch = (size_t)m;
+    uint32_t from = row_at;
+    y += (size_t)(rank * GW) * pitch;
+    for (int g = rank; g < groups; g += split, y += (size_t)(split * GW) * pitch) {
         float sum[GW];
 #pragma unroll
         for (int k = 0; k < GW; ++k) sum[k] = 0.0f;
-        for (int r = 0; r < split; ++r) {
-            const uint32_t from = row_at + (uint32_t)(((g / split) * split + r) * kRows * 4 * GW);
+#pragma unroll 4
+        for (int r = 0; r < split; ++r, from += PLACE) {
             if constexpr (GW == 4) {
                 const uint4 u = lds_v4(from);
                 sum[0] += __uint_as_float(u.x); sum[1] += __uint_as_float(u.y); sum[2] += __uint_as_float(u.z); sum[3] += __uint_as_float(u.w);
@@ -140,9 +167,11 @@ __device__ __forceinline__ bool add_up(const StreamParams &p, uint32_t acc, uint
                 for (int k = 0; k < GW; ++k) sum[k] += __uint_as_float(lds_u32(from + 4 * k));
             }
         }
+        const int left = inside ? tokens - g * GW : 0;
+        T *at = y;
 #pragma unroll
-        for (int k = 0; k < GW; ++k)
-            if (i < p.m && g * GW + k < tokens) store_out(p.y, p.y_f32, (size_t)(tok0 + g * GW + k) * p.m + i, sum[k]);
+        for (int k = 0; k < GW; ++k, at += pitch)
+            if (k < left) put(at, sum[k]);
     }
     return true;
 }
@@ -312,23 +341,19 @@ __global__ void __launch_bounds__(SCfg<BN, QX>::THREADS, 1) lords_mxfp4_stream_k
             tc_fence_after_sync();
             const int ri = q * 32 + lane, i = row0 + ri;
             const uint32_t acc = tmem_base + ((uint32_t)(q * 32) << 16);
-            if (split > 1) {
-                const bool ok = gw == 4   ? add_up<BN, 4>(p, acc, recv, bar_recv, rank, split, tokens, tok0, ri, i, failed)
-                                : gw == 2 ? add_up<BN, 2>(p, acc, recv, bar_recv, rank, split, tokens, tok0, ri, i, failed)
-                                          : add_up<BN, 1>(p, acc, recv, bar_recv, rank, split, tokens, tok0, ri, i, failed);
-                failed = failed || !ok;
-            } else if (!failed) {
-#pragma unroll 1
-                for (int c0 = 0; c0 < tokens; c0 += 16) {
-                    uint32_t v[16];
-                    tmem_ld_32x16(acc + (uint32_t)c0, v);
-                    tmem_wait_ld(v);
-                    if (i < p.m)
-#pragma unroll
-                        for (int c = 0; c < 16; ++c)
-                            if (c0 + c < tokens) store_out(p.y, p.y_f32, (size_t)(tok0 + c0 + c) * p.m + i, __uint_as_float(v[c]));
+            auto out = [&](auto *base) {
+                auto *y = base + (size_t)tok0 * p.m + i;
+                if (split <= 1) {
+                    if (!failed) write_out<BN>(acc, tokens, y, p.m, i < p.m);
+                    return;
                 }
-            }
+                const bool ok = gw == 4   ? add_up<BN, 4>(acc, recv, bar_recv, rank, split, tokens, y, p.m, i < p.m, ri, status, failed)
+                                : gw == 2 ? add_up<BN, 2>(acc, recv, bar_recv, rank, split, tokens, y, p.m, i < p.m, ri, status, failed)
+                                          : add_up<BN, 1>(acc, recv, bar_recv, rank, split, tokens, y, p.m, i < p.m, ri, status, failed);
+                failed = failed || !ok;
+            };
+            if (p.y_f32) out(static_cast<float *>(p.y));
+            else out(static_cast<__nv_bfloat16 *>(p.y));
         }
     }
     if (split > 1 && warp < kConvWarp0) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
