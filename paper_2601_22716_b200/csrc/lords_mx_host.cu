@@ -26,8 +26,8 @@ static bool few_tokens(const MxProblem &p, const State &st)
 {
     if (st.forced_path == 2) return true;
     if (st.forced_path == 8) return false;
-    // Up to 32 tokens the one was never slower, from 513 on the other; between, by their estimates: 128 tokens, 14336 x 4096 15.7 us and 12.0, 4096 x
-    // 4096 9.1 and 9.5; 256 tokens, 4096 x 4096 12.8 and 9.9, 1024 x 4096 7.7 and 8.9.
+    // Up to 32 tokens the one was never slower, from 513 on the other; between, by their estimates: 128 tokens, 14336 x 4096 9.3 us and 11.3, 4096 x
+    // 4096 6.5 and 7.8; 256 tokens, 14336 x 4096 17.8 and 11.8, 4096 x 4096 8.4 and 7.9, 1024 x 4096 6.1 and 7.6.
     return p.M <= 32 || (p.M <= 512 && mxfp4_stream_us(p, st) <= mxfp4_pair_us(p, st));
 }
 

@@ -373,13 +373,15 @@ template <int BN> int run_pair(const MxProblem &p, State &st, cudaStream_t strea
 }  // namespace
 
 // Microseconds of a launch with W from memory: its fixed part, and waves of tiles with a step's and a tile's own (2048 tokens, 14336 x 4096, 4096 x
-// 14336, 4096 x 4096, the weight gradients of 512 and 2048 tokens; y in 32 bits leaves more slowly than the next tile's MMAs take).
+// 14336, 4096 x 4096, the weight gradients of 512 and 2048 tokens; y in 32 bits leaves more slowly than the next tile's MMAs take; fewer tiles than
+// pairs: 64 tokens, 1024 x 1024 4.1, 4096 x 4096 7.4).
 static double pair_us(const MxProblem &p, int bn, int pairs)
 {
     const double steps = (p.n + 255) / 256;
     const long long tiles = (long long)((p.M + kPTokens - 1) / kPTokens) * ((p.m + bn - 1) / bn);
     const double waves = (double)((tiles + pairs - 1) / pairs);
-    return bn == 256 ? 4.7 + waves * (0.36 * steps + (p.y_f32 ? 2.0 : 0.7)) : 4.0 + waves * (0.29 * steps + (p.y_f32 ? 0.6 : 0.42));
+    if (bn == 256) return 4.7 + waves * (0.36 * steps + (p.y_f32 ? 2.0 : 0.7));
+    return 2.6 + 1.4 * (double)(tiles < pairs ? tiles : pairs) / pairs + waves * (0.29 * steps + (p.y_f32 ? 0.6 : 0.42));
 }
 
 double mxfp4_pair_us(const MxProblem &p, const State &st)

@@ -411,15 +411,18 @@ template <int BN, int QX> struct StreamVariant {
         }
         return c > 0 ? c : 0;
     }
-    // CTAs that share a tile's steps: the least waves x (steps of a CTA + a fixed part worth four).
-    static int choose_split(int tiles, int steps, const State &st)
+    // CTAs that share a tile's steps: the least waves x (steps of a CTA + a fixed part worth four + what joining the sums takes, a step and a twentieth for
+    // every token).  64 tokens, 1024 x 1024: 3.3 us on one CTA, 4.1 on two; 1024 x 2048 4.4 and on four 3.9; 128 tokens, 4096 x 1024 4.1 and on two
+    // 5.9.  Up to 32 tokens without that last part, which is small, so that more layers have few enough steps a CTA to take x in bf16.
+    static int choose_split(int tiles, int steps, int tokens, const State &st)
     {
+        const int joining = tokens > 32 ? 20 + tokens : 0;
         int best = 0;
         long long least = 0;
         for (int c = 1; c <= kSplitMax && (c == 1 || 2 * c <= steps); ++c) {
             const int n = resident(c, st);
             if (n < 1) continue;
-            const long long t = (long long)((tiles + n - 1) / n) * ((steps + c - 1) / c + 4);
+            const long long t = (long long)((tiles + n - 1) / n) * (20 * ((steps + c - 1) / c + 4) + (c > 1 ? joining : 0));
             if (best == 0 || t < least) { best = c; least = t; }
         }
         return best;
@@ -428,7 +431,7 @@ template <int BN, int QX> struct StreamVariant {
     {
         const int row_tiles = (k.m + kRows - 1) / kRows, tok_tiles = (k.M + BN - 1) / BN;
         // (the same for every kind of x: sums are in the same order then)
-        const int split = StreamVariant<BN, 0>::choose_split(row_tiles * tok_tiles, k.steps, st);
+        const int split = StreamVariant<BN, 0>::choose_split(row_tiles * tok_tiles, k.steps, k.M < BN ? k.M : BN, st);
         if (split < 1) return LORDS_ERR_UNSUPPORTED;
         if (tok_tiles > 65535) return LORDS_ERR_SHAPE;
         const int own = (k.steps + split - 1) / split;
@@ -451,17 +454,20 @@ template <int BN, int QX> struct StreamVariant {
 template <int BN> double stream_us(const MxProblem &p, const State &st)
 {
     const int steps = (p.n + kStep - 1) / kStep, tiles = (p.m + kRows - 1) / kRows * ((p.M + BN - 1) / BN);
-    const int split = StreamVariant<BN, 0>::choose_split(tiles, steps, st), n = split > 0 ? StreamVariant<BN, 0>::resident(split, st) : 0;
+    const int tokens = p.M < BN ? p.M : BN, split = StreamVariant<BN, 0>::choose_split(tiles, steps, tokens, st);
+    const int n = split > 0 ? StreamVariant<BN, 0>::resident(split, st) : 0;
     if (n < 1) return 1e30;
-    const double waves = (double)((tiles + n - 1) / n), own = (steps + split - 1) / split, tokens = p.M < BN ? p.M : BN;
-    return 1.6 + waves * ((BN <= 64 ? 0.45 : 0.5) * own + 1.0) + (BN <= 64 ? 0.02 : 0.036) * tokens;
+    // a step: the MMAs, or a CTA's share of 5.4 TB/s; launch, set-up and epilogue: 1.75 us, with sums to be joined 1.95
+    const double waves = (double)((tiles + n - 1) / n), own = (steps + split - 1) / split, load = 0.0032 * (tiles < n ? tiles : n) * split;
+    const double mma = BN <= 64 ? 0.29 : 0.33, step = load > mma ? load : mma;
+    return (split > 1 ? 0.95 + 0.021 * tokens : 0.75 + 0.007 * tokens) + waves * (step * own + 1.0);
 }
 
 int tile_for(int M) { return M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : 128; }
 
 }  // namespace
 
-// Estimate in microseconds with x in 4 bits, fitted to four layers at 17 to 300 tokens (within 10 % on most, 25 % at worst).
+// Estimate in microseconds with x in 4 bits, fitted to fourteen layers at 4 to 256 tokens (within 10 % on nearly all, 15 % at worst).
 double mxfp4_stream_us(const MxProblem &p, const State &st)
 {
     switch (tile_for(p.M)) {
