@@ -117,6 +117,8 @@ template <int BN, class T> __device__ __forceinline__ void write_out(uint32_t ac
 }
 
 // The cluster's sums: tokens in groups of GW, group g to rank g mod cluster; a received value's place is (group / cluster, rank, row).
+// (64 tokens of 1024 x 1024 on two CTAs 4.1 us.  Level or slower: the tokens on eight warps, all ranks' values loaded at once; by copies in bulk from
+// shared memory, with a wait for them at the end, 4.45.)
 template <int BN, int GW, class T>
 __device__ __forceinline__ bool add_up(uint32_t acc, uint32_t recv, uint32_t bar_recv, int rank, int split, int tokens, T *y, int m, bool inside, int ri,
                                        const int *status, bool failed)
