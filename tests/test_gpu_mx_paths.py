@@ -99,6 +99,50 @@ def test_a_layer_s_token_counts_agree():
         assert torch.equal(a, b), M
 
 
+@pytest.mark.parametrize("captured", [False, True])
+def test_weights_written_right_before_the_layer(captured):
+    """Neither of the layer's launches reads W before what came ahead of them has ended, a copy and the quantisation of the new weights included."""
+    m, n = 4096, 4096
+    gen = torch.Generator(device="cuda").manual_seed(11)
+    ws = [(torch.randn(m, n, generator=gen, device="cuda") * 0.05).to(torch.bfloat16) for _ in range(3)]
+    four, w = _four(m, n), torch.empty(m, n, dtype=torch.bfloat16, device="cuda")
+    for M in (8, 24, 64, 100):
+        x = torch.randn(M, n, generator=gen, device="cuda").to(torch.bfloat16)
+        want = []
+        for v in ws:
+            q, y = _four(m, n), torch.empty(M, m, dtype=torch.bfloat16, device="cuda")
+            lords.lords_mxfp4_quantize(v, m, n, *q)
+            torch.cuda.synchronize()
+            lords.lords_mxfp4_forward(x, *q, M, m, n, y)
+            torch.cuda.synchronize()
+            want.append(y)
+        got = [torch.empty(M, m, dtype=torch.bfloat16, device="cuda") for _ in range(12)]
+        stream = torch.cuda.Stream()
+
+        def chain():
+            for k, y in enumerate(got):
+                if k % 2:
+                    w.copy_(ws[k % 3])
+                    lords.lords_mxfp4_quantize(w, m, n, *four)
+                else:
+                    lords.lords_mxfp4_quantize(ws[k % 3], m, n, *four)
+                lords.lords_mxfp4_forward(x, *four, M, m, n, y)
+
+        stream.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(stream):
+            if captured:
+                graph = torch.cuda.CUDAGraph()
+                with torch.cuda.graph(graph, stream=stream):
+                    chain()
+            for _ in range(10):
+                for y in got:
+                    y.zero_()
+                graph.replay() if captured else chain()
+                torch.cuda.synchronize()
+                for k, y in enumerate(got):
+                    assert torch.equal(y, want[k % 3]), (M, k)
+
+
 @pytest.mark.parametrize("m,n", [(129, 40), (300, 256), (640, 700), (260, 1000), (1000, 2731), (4096, 4096), (5000, 513), (70, 12000), (20000, 256)])
 def test_a_layer_on_one_launch_or_two(m, n):
     """Few steps a CTA: x is converted inside the product's launch up to 64 tokens x steps, by a launch of its own above; both have the same bits."""
