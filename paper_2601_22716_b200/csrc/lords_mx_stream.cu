@@ -57,7 +57,7 @@ template <int BN, int QX> struct SCfg {
     static constexpr int XRING = QX ? BATCHES * BATCH * XSTEP : 0;
     static constexpr int BARS = 16 * kStagesMax + 16 + 16 * BATCHES + 8;
     static constexpr int FIXED = 1024 + XRING + (BARS + 255) / 256 * 256;      // shared memory apart from stages and partial sums
-    static constexpr int SMEM = 232448;
+    static constexpr int SMEM = 232448, SMEM_SM = 233472;
     static constexpr uint32_t ACC = BN < 32 ? 32 : BN;              // accumulator columns; behind them two sets of scales
     static constexpr uint32_t TMEM = ACC + 32 <= 64 ? 64 : ACC + 32 <= 128 ? 128 : 256;
     static_assert(STAGE % 1024 == 0 && XSTEP % 1024 == 0, "tiles begin at 1024 bytes");
@@ -443,6 +443,12 @@ template <int BN, int QX> struct StreamVariant {
         // (with x in bf16, more loads of W in flight hold up those of x: 14336 x 4096, one token 9.1 us with five to seven stages, 9.7 with twelve, 9.5 with four)
         constexpr int most = QX > 0 ? 6 : kStagesMax;
         if (k.stages > most) k.stages = most;
+        // More tiles than are resident: two CTAs to an SM, so that one's set-up and epilogue run beside the other's loads (28672 x 4096, one token 16.2 us
+        // on one, 13.3 so; 65536 x 4096 33.8 and 26.7; 32000 x 1024, 128 tokens 9.0 and 5.9).
+        if (row_tiles * tok_tiles > StreamVariant<BN, 0>::resident(split, st)) {
+            const int two = (C::SMEM_SM / 2 - 1024 - C::FIXED - sums) / C::STAGE;
+            if (two >= 2 && k.stages > two) k.stages = two;
+        }
         if (QX > 0 && k.M * (QX == 4 && own > C::BATCH ? C::BATCH : own) > C::WORK) return LORDS_ERR_UNSUPPORTED;
         cudaLaunchConfig_t cfg;
         cudaLaunchAttribute attr[2];
@@ -460,17 +466,18 @@ template <int BN> double stream_us(const MxProblem &p, const State &st)
     const int tokens = p.M < BN ? p.M : BN, split = StreamVariant<BN, 0>::choose_split(tiles, steps, tokens, st);
     const int n = split > 0 ? StreamVariant<BN, 0>::resident(split, st) : 0;
     if (n < 1) return 1e30;
-    // a step: the MMAs, or a CTA's share of 5.4 TB/s; launch, set-up and epilogue: 1.75 us, with sums to be joined 1.95
-    const double waves = (double)((tiles + n - 1) / n), own = (steps + split - 1) / split, load = 0.0032 * (tiles < n ? tiles : n) * split;
-    const double mma = BN <= 64 ? 0.29 : 0.33, step = load > mma ? load : mma;
-    return (split > 1 ? 0.95 + 0.021 * tokens : 0.75 + 0.007 * tokens) + waves * (step * own + 1.0);
+    // W from memory at 5.4 TB/s or the busiest SM's MMAs; set-up and epilogue of each round (two CTAs an SM if one is not enough), more of it with sums to be
+    // joined; the launch
+    const double waves = (double)((tiles + n - 1) / n), rounds = tiles > n ? (double)((tiles + 2 * n - 1) / (2 * n)) : 1.0;
+    const double load = 0.0032 * steps * ((p.m + kRows - 1) / kRows), mma = waves * ((steps + split - 1) / split) * (BN <= 64 ? 0.29 : 0.33);
+    return (load > mma ? load : mma) + rounds * (split > 1 ? 2.7 + 0.021 * tokens : 2.5 + 0.007 * tokens) - 0.75;
 }
 
 int tile_for(int M) { return M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : 128; }
 
 }  // namespace
 
-// Estimate in microseconds with x in 4 bits, fitted to fourteen layers at 4 to 256 tokens (within 10 % on nearly all, 15 % at worst).
+// Estimate in microseconds with x in 4 bits, fitted to some twenty layers at 4 to 512 tokens (within 10 % on nearly all, 15 % at worst).
 double mxfp4_stream_us(const MxProblem &p, const State &st)
 {
     switch (tile_for(p.M)) {
