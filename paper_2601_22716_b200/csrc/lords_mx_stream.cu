@@ -100,6 +100,14 @@ template <int GW> __device__ __forceinline__ void send(uint32_t addr, const uint
 __device__ __forceinline__ void put(float *at, float v) { *at = v; }
 __device__ __forceinline__ void put(__nv_bfloat16 *at, float v) { *at = __float2bfloat16_rn(v); }
 
+// The epilogue's four warps have taken the sums from TMEM, which the warp that allocated it may return.
+__device__ __forceinline__ void sums_read()
+{
+    __syncwarp();
+    tc_fence_before_sync();
+    asm volatile("bar.sync 1, 160;" ::: "memory");
+}
+
 // The sums of a row (y: where its value of token 0 goes, `inside`: it is a row of W) as the one CTA of a tile has them.
 template <int BN, class T> __device__ __forceinline__ void write_out(uint32_t acc, int tokens, T *y, int m, bool inside)
 {
@@ -150,6 +158,7 @@ __device__ __forceinline__ bool add_up(uint32_t acc, uint32_t recv, uint32_t bar
             if (++to == split) { to = 0; where += (uint32_t)split * PLACE; }
         }
     }
+    sums_read();
     if (rank >= groups) return true;
     if (!__all_sync(0xffffffffu, mbar_wait_cluster(bar_recv, 0, status, 65))) return false;
     if (failed) return true;
@@ -211,13 +220,17 @@ __global__ void __launch_bounds__(SCfg<BN, QX>::THREADS, 1) lords_mxfp4_stream_k
             tma_prefetch_desc(&p.tm_w);
             if (!QX) tma_prefetch_desc(&p.tm_x);
         }
-    } else if (warp == 2) {
+        __syncwarp();
+    }
+    // No CTA waits for another of its cluster while it holds TMEM: beside clusters of another stream that do the same each could hold what the other waits
+    // for.  So it says that its barriers exist before it asks for TMEM, and returns that before it waits for the others' sums.
+    if (split > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");      // waited for before the first store to another CTA
+    if (warp == 2) {
         tmem_alloc(tmem_slot, C::TMEM);
         tmem_relinquish();
     }
     tc_fence_before_sync();
     __syncthreads();
-    if (split > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");      // waited for before the first store to another CTA
     tc_fence_after_sync();
     uint32_t tmem_base;
     asm volatile("ld.shared.u32 %0, [%1];" : "=r"(tmem_base) : "r"(tmem_slot));
@@ -348,6 +361,7 @@ __global__ void __launch_bounds__(SCfg<BN, QX>::THREADS, 1) lords_mxfp4_stream_k
                 auto *y = base + (size_t)tok0 * p.m + i;
                 if (split <= 1) {
                     if (!failed) write_out<BN>(acc, tokens, y, p.m, i < p.m);
+                    sums_read();
                     return;
                 }
                 const bool ok = gw == 4   ? add_up<BN, 4>(acc, recv, bar_recv, rank, split, tokens, y, p.m, i < p.m, ri, status, failed)
@@ -359,15 +373,13 @@ __global__ void __launch_bounds__(SCfg<BN, QX>::THREADS, 1) lords_mxfp4_stream_k
             else out(static_cast<__nv_bfloat16 *>(p.y));
         }
     }
-    if (split > 1 && warp < kConvWarp0) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-
-    if (failed) ptx::record_give_up(p.status, LORDS_ERR_TIMEOUT);
-    tc_fence_before_sync();
-    __syncthreads();
     if (warp == 2) {
+        sums_read();
         tc_fence_after_sync();
         tmem_dealloc(tmem_base, C::TMEM);
     }
+    if (split > 1 && warp < kConvWarp0) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    if (failed) ptx::record_give_up(p.status, LORDS_ERR_TIMEOUT);
 }
 
 template <int BN, int QX> struct StreamVariant {
