@@ -13,7 +13,7 @@
 // do not touch each other.
 //
 // Bound: the stream of codes and scales, 17/32 bytes a weight, behind some 2.4 us of launch, set-up and epilogue: 14336 x 4096, one token, codes given
-// 7.9 us, of which the loads alone 7.5 (31 MB in 5.1 us, 6.1 TB/s); with x in bf16 8.5.  4096 x 4096: 3.7 and 4.4.  Everything is read in the
+// 7.9 us, of which the loads alone 7.5 (31 MB in 5.1 us, 6.1 TB/s); with x in bf16 8.5.  4096 x 4096: 3.4 and 4.4.  Everything is read in the
 // stream's order.  (Asking L2 for the first tiles of W ahead of the previous launch's end: 8.3 -> 8.0 us, but 4.0 -> 4.15 for the smaller layer and
 // 9.8 with all tiles; CTAs small enough for two on an SM 9.0: both against the kernel before its last steps.  Reading W while the launch before
 // converts x, which then has to hold this one back until all before it has ended: 8 tokens 9.5 -> 10.5, 32 tokens of 4096 x 4096 5.8 -> 6.3.)
@@ -126,7 +126,7 @@ template <int BN, class T> __device__ __forceinline__ void write_out(uint32_t ac
 }
 
 // The cluster's sums: tokens in groups of GW, group g to rank g mod cluster; a received value's place is (group / cluster, rank, row).
-// (64 tokens of 1024 x 1024 on two CTAs 4.1 us.  Level or slower: the tokens on eight warps, all ranks' values loaded at once; by copies in bulk from
+// (64 tokens of 1024 x 1024 on two CTAs 4.1 us, 3.3 on one.  Level or slower: the tokens on eight warps, all ranks' values loaded at once; by copies in bulk from
 // shared memory, with a wait for them at the end, 4.45.)
 template <int BN, int GW, class T>
 __device__ __forceinline__ bool add_up(uint32_t acc, uint32_t recv, uint32_t bar_recv, int rank, int split, int tokens, T *y, int m, bool inside, int ri,
