@@ -99,6 +99,31 @@ def test_a_layer_s_token_counts_agree():
         assert torch.equal(a, b), M
 
 
+def test_clusters_of_several_streams_share_the_sms():
+    """Calls of four token counts at once, each a cluster's: CTAs of different tiles lie on the same SMs and use their tensor memory together."""
+    m, n = 1024, 4096
+    counts = (1, 16, 64, 128)
+    _, wq, _ = _operand(m, n, 5, 0.05)
+    args, want = [], []
+    for k, M in enumerate(counts):
+        x, xq, _ = _operand(M, n, 20 + k)
+        args.append((x, *wq) if M == 1 else (*xq, *wq))
+        want.append(torch.empty(M, m, device="cuda"))
+    calls = [lords.lords_mxfp4_forward if M == 1 else lords.lords_mxfp4_matmul for M in counts]
+    for f, a, M, y in zip(calls, args, counts, want):
+        f(*a, M, m, n, y, f32=True)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in counts]
+    got = [[torch.empty_like(y) for _ in range(50)] for y in want]
+    torch.cuda.synchronize()
+    for r in range(50):
+        for k, M in enumerate(counts):
+            calls[k](*args[k], M, m, n, got[k][r], stream=streams[k], f32=True)
+    torch.cuda.synchronize()
+    assert lords.lords_poll_status() == 0
+    assert all(torch.equal(y, want[k]) for k in range(len(counts)) for y in got[k])
+
+
 @pytest.mark.parametrize("captured", [False, True])
 def test_weights_written_right_before_the_layer(captured):
     """Neither of the layer's launches reads W before what came ahead of them has ended, a copy and the quantisation of the new weights included."""
