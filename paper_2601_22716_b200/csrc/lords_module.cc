@@ -65,8 +65,8 @@ bool to_int(PyObject *o, int *v)
     int overflow = 0;
     const long l = PyLong_AsLongAndOverflow(o, &overflow);
     if (l == -1 && PyErr_Occurred()) return false;
-    // what no int holds is out of every range as well: the call refuses it
-    *v = overflow > 0 || l > INT_MAX ? INT_MAX : overflow < 0 || l < INT_MIN ? INT_MIN : (int)l;
+    // what no int holds becomes a size that every call refuses (m has no upper limit in the calls on packed codes: a large number would pass)
+    *v = overflow != 0 || l > INT_MAX || l < INT_MIN ? INT_MIN : (int)l;
     return true;
 }
 
