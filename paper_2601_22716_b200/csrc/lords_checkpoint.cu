@@ -21,7 +21,7 @@ constexpr int kStoreRows = 2;               // rows a warp of the store (four: 2
 template <int PER>
 __global__ void __launch_bounds__(kCThreads) lords_checkpoint_store_kernel(const uint16_t *x, int M, int n, int qp, int ep, int wide, uint8_t *q, uint8_t *e)
 {
-    const int lane = threadIdx.x & 31, t0 = ((int)blockIdx.y * (kCThreads / 32) + (threadIdx.x >> 5)) * PER;
+    const int lane = threadIdx.x & 31, t0 = (row_block() * (kCThreads / 32) + (threadIdx.x >> 5)) * PER;
     const int c = (int)blockIdx.x * 512 + lane * 16;
     const uint16_t *end = x + (size_t)M * n;
     ptx::griddep_launch_dependents();
@@ -92,7 +92,7 @@ template <int PER, bool WIDE>
 __global__ void __launch_bounds__(kCThreads) lords_checkpoint_load_kernel(const uint8_t *q, const uint8_t *e, int M, int n, int qp, int ep, uint16_t *x)
 {
     constexpr int VALUES = WIDE ? 16 : 8;
-    const int lane = threadIdx.x & 31, t0 = ((int)blockIdx.y * (kCThreads / 32) + (threadIdx.x >> 5)) * PER;
+    const int lane = threadIdx.x & 31, t0 = (row_block() * (kCThreads / 32) + (threadIdx.x >> 5)) * PER;
     const int c = ((int)blockIdx.x * 32 + lane) * VALUES;
     ptx::griddep_launch_dependents();
     ptx::griddep_wait();
@@ -128,7 +128,7 @@ __global__ void __launch_bounds__(kCThreads) lords_checkpoint_load_kernel(const 
 
 // One row a warp where more would leave fewer than two CTAs an SM.
 bool small(int M, int n, int cols, int per) { return (long long)((M + 8 * per - 1) / (8 * per)) * ((n + cols - 1) / cols) < 296; }
-dim3 grid_of(int M, int n, int cols, int per) { return dim3((unsigned)((n + cols - 1) / cols), (unsigned)((M + 8 * per - 1) / (8 * per))); }
+dim3 grid_of(int M, int n, int cols, int per) { return mx::grid_of((unsigned)((n + cols - 1) / cols), (unsigned)((M + 8 * per - 1) / (8 * per))); }
 
 }  // namespace
 

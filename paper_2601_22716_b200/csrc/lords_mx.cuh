@@ -25,6 +25,14 @@ __host__ __device__ inline int blocks_of(int cols) { return (cols + kBlock - 1) 
 __host__ __device__ inline int scale_tiles_of(int cols) { return (blocks_of(cols) + kTileBlocks - 1) / kTileBlocks; }
 __host__ __device__ inline size_t codes_pitch(int cols) { return (size_t)blocks_of(cols) * 16; }
 
+// Blocks of rows on the grid's y axis, which ends at 65535, and on z behind it.
+inline dim3 grid_of(unsigned col_blocks, unsigned row_blocks)
+{
+    const unsigned z = (row_blocks + 65534u) / 65535u;
+    return dim3(col_blocks, (row_blocks + z - 1) / z, z);
+}
+__device__ __forceinline__ int row_block() { return (int)(blockIdx.z * gridDim.y + blockIdx.y); }
+
 // Where the scale of row i and block b of a tile lies inside it: four words a lane, a word the four blocks of row 32 j + lane.
 __host__ __device__ inline int scale_at(int i, int b) { return (i & 31) * 16 + (i >> 5) * 4 + b; }
 

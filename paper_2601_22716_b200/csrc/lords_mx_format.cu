@@ -173,7 +173,7 @@ __global__ void __launch_bounds__(kDThreads) lords_mxfp4_dequantize_kernel(const
 {
     constexpr int ROWS = WIDE ? 2 : 4, PER = WIDE ? 16 : 8;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int c = ((int)blockIdx.x * 32 + lane) * PER, r0 = ((int)blockIdx.y * (kDThreads / 32) + warp) * ROWS, b = c / kBlock;
+    const int c = ((int)blockIdx.x * 32 + lane) * PER, r0 = (row_block() * (kDThreads / 32) + warp) * ROWS, b = c / kBlock;
     ptx::griddep_launch_dependents();
     ptx::griddep_wait();
     // (the rows lie in one row of tiles)
@@ -227,12 +227,12 @@ int launch_mxfp4_quantize(const uint16_t *v, int rows, int cols, uint8_t *codes,
 int launch_mxfp4_dequantize(const uint8_t *codes, const uint8_t *scales, int rows, int cols, uint16_t *v, cudaStream_t stream)
 {
     const int pitch = (int)codes_pitch(cols), ktiles = scale_tiles_of(cols);
-    if (cols % 16 == 0 && reinterpret_cast<uintptr_t>(v) % 32 == 0) {
-        const dim3 grid((unsigned)((cols + 511) / 512), (unsigned)((rows + 15) / 16));
-        return launch_dependent(lords_mxfp4_dequantize_kernel<true>, grid, kDThreads, stream, codes, scales, rows, cols, pitch, ktiles, v);
-    }
-    const dim3 grid((unsigned)((cols + 255) / 256), (unsigned)((rows + 31) / 32));
-    return launch_dependent(lords_mxfp4_dequantize_kernel<false>, grid, kDThreads, stream, codes, scales, rows, cols, pitch, ktiles, v);
+    auto launch = [&](auto kernel, int across, int down) {
+        return launch_dependent(kernel, grid_of((unsigned)((cols + across - 1) / across), (unsigned)((rows + down - 1) / down)), kDThreads, stream, codes, scales, rows,
+                                cols, pitch, ktiles, v);
+    };
+    if (cols % 16 == 0 && reinterpret_cast<uintptr_t>(v) % 32 == 0) return launch(lords_mxfp4_dequantize_kernel<true>, 512, 16);
+    return launch(lords_mxfp4_dequantize_kernel<false>, 256, 32);
 }
 
 }  // namespace lords
