@@ -206,7 +206,7 @@ __global__ void __launch_bounds__(SCfg<BN, QX>::THREADS, 1) lords_mxfp4_stream_k
     const int tokens = p.M - tok0 < BN ? p.M - tok0 : BN;
     const int gw = group_of(tokens);
     const int *status = p.status;
-    bool failed = false;
+    bool failed = false, alone = false;
 
     if (warp == 0) {
         if (lane == 0) {
@@ -367,7 +367,8 @@ __global__ void __launch_bounds__(SCfg<BN, QX>::THREADS, 1) lords_mxfp4_stream_k
                 const bool ok = gw == 4   ? add_up<BN, 4>(acc, recv, bar_recv, rank, split, tokens, y, p.m, i < p.m, ri, status, failed)
                                 : gw == 2 ? add_up<BN, 2>(acc, recv, bar_recv, rank, split, tokens, y, p.m, i < p.m, ri, status, failed)
                                           : add_up<BN, 1>(acc, recv, bar_recv, rank, split, tokens, y, p.m, i < p.m, ri, status, failed);
-                failed = failed || !ok;
+                alone = !ok;
+                failed = failed || alone;
             };
             if (p.y_f32) out(static_cast<float *>(p.y));
             else out(static_cast<__nv_bfloat16 *>(p.y));
@@ -379,7 +380,15 @@ __global__ void __launch_bounds__(SCfg<BN, QX>::THREADS, 1) lords_mxfp4_stream_k
         tmem_dealloc(tmem_base, C::TMEM);
     }
     if (split > 1 && warp < kConvWarp0) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-    if (failed) ptx::record_give_up(p.status, LORDS_ERR_TIMEOUT);
+    if (failed) {
+        ptx::record_give_up(p.status, LORDS_ERR_TIMEOUT);
+        // A CTA whose wait for the others' sums gave up holds its shared memory until they have stored theirs, or have left: a thread that has exited counts
+        // as arrived, and the waits of the others are bounded.
+        if (alone) {
+            asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+            asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+        }
+    }
 }
 
 template <int BN, int QX> struct StreamVariant {
