@@ -100,12 +100,24 @@ template <int GW> __device__ __forceinline__ void send(uint32_t addr, const uint
 __device__ __forceinline__ void put(float *at, float v) { *at = v; }
 __device__ __forceinline__ void put(__nv_bfloat16 *at, float v) { *at = __float2bfloat16_rn(v); }
 
-// The epilogue's four warps have taken the sums from TMEM, which the warp that allocated it may return.
-__device__ __forceinline__ void sums_read()
+// The epilogue's four warps have taken the sums from TMEM, and the issuer has issued its last MMA: the warp that allocated TMEM may return it.  Returns
+// whether any of them waited for the MMAs in vain, which may then still be at work.
+__device__ __forceinline__ bool sums_read(bool in_vain)
 {
     __syncwarp();
     tc_fence_before_sync();
-    asm volatile("bar.sync 1, 160;" ::: "memory");
+    uint32_t any;
+    asm volatile(
+        "{\n"
+        ".reg .pred p, q;\n"
+        "setp.ne.u32 p, %1, 0;\n"
+        "bar.red.or.pred q, 1, 192, p;\n"
+        "selp.u32 %0, 1, 0, q;\n"
+        "}\n"
+        : "=r"(any)
+        : "r"((uint32_t)in_vain)
+        : "memory");
+    return any != 0u;
 }
 
 // The sums of a row (y: where its value of token 0 goes, `inside`: it is a row of W) as the one CTA of a tile has them.
@@ -140,8 +152,13 @@ __device__ __forceinline__ bool add_up(uint32_t acc, uint32_t recv, uint32_t bar
 #pragma unroll 1
     for (int c0 = 0; c0 < tokens; c0 += 16) {
         uint32_t v[16];
-        tmem_ld_32x16(acc + (uint32_t)c0, v);
-        tmem_wait_ld(v);
+        if (!failed) {
+            tmem_ld_32x16(acc + (uint32_t)c0, v);
+            tmem_wait_ld(v);
+        } else {                       // MMAs may still write them: the others get zeros, so that their waits end
+#pragma unroll
+            for (int c = 0; c < 16; ++c) v[c] = 0u;
+        }
 #pragma unroll
         for (int c = 0; c < 16 && (GW == 4 || c == 0); c += GW) {
             if (c0 + c >= tokens) break;
@@ -158,7 +175,7 @@ __device__ __forceinline__ bool add_up(uint32_t acc, uint32_t recv, uint32_t bar
             if (++to == split) { to = 0; where += (uint32_t)split * PLACE; }
         }
     }
-    sums_read();
+    sums_read(failed);
     if (rank >= groups) return true;
     if (!__all_sync(0xffffffffu, mbar_wait_cluster(bar_recv, 0, status, 65))) return false;
     if (failed) return true;
@@ -290,6 +307,7 @@ __global__ void __launch_bounds__(SCfg<BN, QX>::THREADS, 1) lords_mxfp4_stream_k
             if (QX && it % kBatch == kBatch - 1) umma_commit(bar_x_free + 8 * (batch % kBatches), leader);
         }
         umma_commit(bar_acc, leader);
+        sums_read(false);
     } else if (warp >= kConvWarp0) {
         if constexpr (QX > 0) {
             // -------------------------------------------------------------- x to 4 bits, a block at a time, a batch of steps after the other.  (Tokens
@@ -361,7 +379,7 @@ __global__ void __launch_bounds__(SCfg<BN, QX>::THREADS, 1) lords_mxfp4_stream_k
                 auto *y = base + (size_t)tok0 * p.m + i;
                 if (split <= 1) {
                     if (!failed) write_out<BN>(acc, tokens, y, p.m, i < p.m);
-                    sums_read();
+                    sums_read(failed);
                     return;
                 }
                 const bool ok = gw == 4   ? add_up<BN, 4>(acc, recv, bar_recv, rank, split, tokens, y, p.m, i < p.m, ri, status, failed)
@@ -375,7 +393,8 @@ __global__ void __launch_bounds__(SCfg<BN, QX>::THREADS, 1) lords_mxfp4_stream_k
         }
     }
     if (warp == 2) {
-        sums_read();
+        // (After a wait in vain the MMAs end soon after the last one has been issued.  A wait in every call: 256 x 256, four tokens 0.1 us more.)
+        if (sums_read(false) && !mbar_wait_warp(bar_acc, 0, status, 67)) failed = true;
         tc_fence_after_sync();
         tmem_dealloc(tmem_base, C::TMEM);
     }

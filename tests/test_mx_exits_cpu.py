@@ -58,3 +58,42 @@ def test_a_receiver_stays_while_others_may_send():
 
             broken, stuck = runs(programs, enabled, allowed)
             assert not stuck and not broken, (senders, gave_up_too, broken[:1], stuck[:1])
+
+
+def test_tensor_memory_goes_back_when_nothing_writes_it():
+    """The epilogue's wait for the accumulator gave up while the issuer was still at work: its columns are freed, and read, only when that has ended."""
+    threads = {int(k) for k in re.findall(r"bar\.(?:sync|red\.or\.pred q,) 1, (\d+)", CODE)}
+    assert len(threads) == 1
+    # the roles that meet at the named barrier before the columns are freed: four epilogue warps, the one that frees, and the issuer if it takes part
+    issuer = KERNEL[KERNEL.index("warp == 1"):KERNEL.index("warp >= kConvWarp0", KERNEL.index("warp == 1"))]
+    tail = issuer[issuer.rindex("umma_commit(bar_acc"):]
+    issuer_meets = "sums_read(" in tail
+    assert threads == {32 * (5 + issuer_meets)}
+    free = KERNEL[KERNEL.rindex("sums_read("):KERNEL.rindex("tmem_dealloc(")]
+    waits = re.search(r"mbar_wait_warp\(bar_acc\b", free) is not None
+    # what the epilogue does once its wait has given up: does it still load the accumulator?
+    reads = [c for c in re.findall(r"([^;{}]*)[;{]\s*tmem_ld_32x16\(", ADD_UP) if "!failed" not in c]
+    programs = {
+        "epilogue": ["give up"] + (["read"] if reads else []) + ["meet"],
+        "issuer": ["issue", "issue again", "commit"] + (["meet"] if issuer_meets else []),
+        "tensor core": ["finish"],                    # the MMAs and copies that the issuer has committed
+        "owner": ["meet", "met"] + (["see them finish"] if waits else []) + ["free"],
+    }
+    meeting = [r for r in programs if "meet" in programs[r]]
+
+    def enabled(role, step, done):
+        if step == "met":
+            return all((r, "meet") in done for r in meeting)
+        if step == "finish":
+            return ("issuer", "commit") in done
+        return step != "see them finish" or ("tensor core", "finish") in done
+
+    def allowed(role, step, done):
+        if step in ("issue", "issue again"):
+            return ("owner", "free") not in done
+        if step in ("read", "free"):                  # while MMAs may write the columns
+            return ("tensor core", "finish") in done
+        return True
+
+    broken, stuck = runs(programs, enabled, allowed)
+    assert not stuck and not broken, (broken[:1], stuck[:1])
