@@ -22,6 +22,8 @@
 #include <cuda.h>
 #include <cuda_bf16.h>
 
+#include <atomic>
+
 #include "lords_internal.h"
 #include "lords_mx.cuh"
 #include "lords_ptx.cuh"
@@ -431,28 +433,32 @@ template <int BN, int QX> struct StreamVariant {
     // The kernel may use its shared memory, once per device.
     static cudaError_t allow(const State &st)
     {
-        static bool done[kMaxDevices] = {};
-        bool &d = done[device_slot(st)];
-        const cudaError_t e = d ? cudaSuccess : cudaFuncSetAttribute(lords_mxfp4_stream_kernel<BN, QX>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
-        d = e == cudaSuccess;
+        static std::atomic<bool> done[kMaxDevices];
+        std::atomic<bool> &d = done[device_slot(st)];
+        if (d.load(std::memory_order_acquire)) return cudaSuccess;
+        const cudaError_t e = cudaFuncSetAttribute(lords_mxfp4_stream_kernel<BN, QX>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
+        if (e == cudaSuccess) d.store(true, std::memory_order_release);
         return e;
     }
-    // Clusters of `split` CTAs that can be resident at once.
+    // Clusters of `split` CTAs that can be resident at once.  (Host threads may ask at the same time: each stores the answer, and nothing before it.)
     static int resident(int split, const State &st)
     {
-        static int cache[kMaxDevices][kSplitMax + 1] = {};
-        int &c = cache[device_slot(st)][split];
-        if (c == 0) {
-            c = -1;
-            if (allow(st) != cudaSuccess) return 0;
+        static std::atomic<int> cache[kMaxDevices][kSplitMax + 1];      // 0: not asked yet, -1: none
+        std::atomic<int> &c = cache[device_slot(st)][split];
+        int known = c.load(std::memory_order_relaxed);
+        if (known == 0) {
             cudaLaunchConfig_t cfg;
             cudaLaunchAttribute attr[2];
             fill(cfg, attr, 1, 1, split, nullptr);
             int n = 0;
-            if (cudaOccupancyMaxActiveClusters(&n, lords_mxfp4_stream_kernel<BN, QX>, &cfg) != cudaSuccess) (void)cudaGetLastError();
-            if (n >= 1) c = n;
+            if (allow(st) != cudaSuccess || cudaOccupancyMaxActiveClusters(&n, lords_mxfp4_stream_kernel<BN, QX>, &cfg) != cudaSuccess) {
+                (void)cudaGetLastError();
+                return 0;
+            }
+            known = n >= 1 ? n : -1;
+            c.store(known, std::memory_order_relaxed);
         }
-        return c > 0 ? c : 0;
+        return known > 0 ? known : 0;
     }
     // CTAs that share a tile's steps: the least waves x (steps of a CTA + a fixed part worth four + what joining the sums takes, a step and a twentieth for
     // every token).  64 tokens, 1024 x 1024: 3.3 us on one CTA, 4.1 on two; 1024 x 2048 4.4 and on four 3.9; 128 tokens, 4096 x 1024 4.1 and on two

@@ -1,4 +1,7 @@
-"""Microscaled formats at the ends of their ranges."""
+"""Microscaled formats at the ends of their ranges, and a process whose first calls come from several threads at once."""
+import subprocess
+import sys
+
 import pytest
 import torch
 
@@ -56,3 +59,50 @@ def test_the_most_rows(rows, cols):
         got, got_q = there_and_back(v, rows, size, to, back)
         assert torch.equal(got, want.repeat(256, 1)[:rows])
         assert torch.equal(got_q, want_q.repeat(256)[:got_q.numel()])
+
+
+FIRST = """
+import threading
+import torch
+from paper_2601_22716_b200 import binding as lords
+M, m, n = {M}, 640, {n}
+lords.lords_init(0, 0)
+gen = torch.Generator(device="cuda").manual_seed(1)
+four = lambda r, c: [torch.empty(f(r, c), dtype=torch.uint8, device="cuda") for f in (lords.lords_mxfp4_codes_bytes, lords.lords_mxfp4_scales_bytes)]
+x, w = (torch.randn(r, n, generator=gen, device="cuda").to(torch.bfloat16) for r in (M, m))
+xq, wq = four(M, n), four(m, n)
+lords.lords_mxfp4_quantize(x, M, n, *xq)
+lords.lords_mxfp4_quantize(w, m, n, *wq)
+count = 8
+streams, ys = [torch.cuda.Stream() for _ in range(count)], [torch.empty(M, m, device="cuda") for _ in range(count)]
+torch.cuda.synchronize()
+gate, bad = threading.Barrier(count), []
+
+def work(k):
+    torch.cuda.set_device(0)
+    gate.wait()
+    try:
+        if M <= 4 and k % 2:         # (no scratch memory: calls on several streams do not meet)
+            lords.lords_mxfp4_forward(x, *wq, M, m, n, ys[k], stream=streams[k], f32=True)
+        else:
+            lords.lords_mxfp4_matmul(*xq, *wq, M, m, n, ys[k], stream=streams[k], f32=True)
+    except Exception as e:
+        bad.append(e)
+
+threads = [threading.Thread(target=work, args=(k,)) for k in range(count)]
+[t.start() for t in threads]
+[t.join() for t in threads]
+torch.cuda.synchronize()
+want = torch.empty(M, m, device="cuda")
+lords.lords_mxfp4_matmul(*xq, *wq, M, m, n, want, f32=True)
+torch.cuda.synchronize()
+assert not bad, bad
+assert lords.lords_poll_status() == 0
+assert all(torch.equal(y, want) for y in ys), [torch.equal(y, want) for y in ys]
+"""
+
+
+@pytest.mark.parametrize("M,n", [(3, 256), (3, 4096), (30, 256), (30, 4096), (100, 4096)])
+def test_first_calls_from_several_threads(M, n):
+    """How many clusters of a kernel fit is asked once; a thread that asks meanwhile gets the same answer."""
+    subprocess.run([sys.executable, "-c", FIRST.format(M=M, n=n)], check=True, timeout=300)
