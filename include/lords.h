@@ -332,10 +332,10 @@ int lords_mxfp4_matmul_f32(const uint8_t *x_codes, const uint8_t *x_scales, cons
 
 /*
  * A layer held in 4 bits: x (bf16 [M][n]) is brought to 4 bits as lords_mxfp4_quantize does it, then y = x W^T as above.  The
- * same results as those two calls, to the last bit.  Up to four tokens it is one launch without scratch memory; above, x in 4 bits may lie in the
- * lords_init workspace (as for the forward calls, two such calls may then only overlap if they are ordered on one stream).  Calls of more than 512
- * tokens for which the workspace is too small go through it part by part; LORDS_ERR_WORKSPACE when it does not hold 128 tokens, or
- * all of a smaller call.
+ * same results as those two calls, to the last bit.  Up to four tokens it is one launch without scratch memory, and up to 64 where n leaves each CTA
+ * few columns; else x in 4 bits lies in the lords_init workspace (as for the forward calls, two such calls may then only overlap if they are ordered on
+ * one stream).  Calls of more than 512 tokens for which the workspace is too small go through it part by part; LORDS_ERR_WORKSPACE when it does not hold
+ * 128 tokens, or all of a smaller call.
  */
 int lords_mxfp4_forward(const void *x, const uint8_t *w_codes, const uint8_t *w_scales, int M, int m, int n, void *y, void *stream);
 int lords_mxfp4_forward_f32(const void *x, const uint8_t *w_codes, const uint8_t *w_scales, int M, int m, int n, float *y32, void *stream);

@@ -61,9 +61,8 @@ static int forward_common(const void *x, const uint8_t *w, const uint8_t *ws, in
     st.last_launches = 0;
     MxProblem p = {static_cast<const uint16_t *>(x), nullptr, nullptr, w, ws, M, m, n, y, y_f32};
     auto room = [&](int tokens) { return ((codes_bytes(tokens, n) + 255) & ~(size_t)255) + scales_bytes(tokens, n); };
-    // One launch, where the kernel takes x in bf16.  (From 17 tokens on only if the workspace would hold x in 4 bits as well: a program that reserves too
-    // little learns it from every layer, not from the ones with many steps alone.)
-    if ((M <= 16 || (M <= 64 && room(M) <= st.workspace_bytes)) && few_tokens(p, st)) {
+    // One launch without scratch memory, where the kernel takes x in bf16.
+    if (M <= 64 && few_tokens(p, st)) {
         rc = launch_mxfp4_stream(p, st, s);
         if (rc != LORDS_ERR_UNSUPPORTED) return rc;
     }

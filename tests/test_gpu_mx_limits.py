@@ -61,6 +61,37 @@ def test_the_most_rows(rows, cols):
         assert torch.equal(got_q, want_q.repeat(256)[:got_q.numel()])
 
 
+@pytest.mark.parametrize("M,n", [(17, 256), (33, 256), (64, 256), (20, 500), (32, 512)])
+def test_a_call_of_one_launch_needs_no_workspace(M, n):
+    """Few columns: x is converted inside the product's launch, so a workspace that would not hold it is no reason to refuse."""
+    m = 384
+    x, w = _normal(M, n, 1), _normal(m, n, 2)
+    xq, wq = _four(M, n), _four(m, n)
+    lords.lords_mxfp4_quantize(x, M, n, *xq)
+    lords.lords_mxfp4_quantize(w, m, n, *wq)
+    want = torch.empty(M, m, device="cuda")
+    lords.lords_mxfp4_matmul(*xq, *wq, M, m, n, want, f32=True)
+    torch.cuda.synchronize()
+    lords.lords_shutdown()
+    try:
+        lords.lords_init(0, 1024)
+        y = torch.empty(M, m, device="cuda")
+        lords.lords_mxfp4_forward(x, *wq, M, m, n, y, f32=True)
+        assert lords.lords_last_launch_count() == 1 and torch.equal(y, want)
+        # two launches, and no room for x between them: refused before anything is written
+        wide = 12000
+        a, b, out = _normal(M, wide, 3), _normal(m, wide, 4), torch.full((M, m), -7.0, device="cuda")
+        bq = _four(m, wide)
+        lords.lords_mxfp4_quantize(b, m, wide, *bq)
+        with pytest.raises(lords.LordsError) as e:
+            lords.lords_mxfp4_forward(a, *bq, M, m, wide, out, f32=True)
+        torch.cuda.synchronize()
+        assert e.value.status == -9 and bool((out == -7.0).all())
+    finally:
+        lords.lords_shutdown()
+        lords.lords_init(0, 0)
+
+
 FIRST = """
 import threading
 import torch
