@@ -349,10 +349,10 @@ int lords_checkpoint_store(const void *x, int M, int n, uint8_t *q, uint8_t *e, 
 int lords_checkpoint_load(const uint8_t *q, const uint8_t *e, int M, int n, void *x, void *stream);
 
 /*
- * lords_linear_backward_factors and lords_linear_backward_qat with the layer's input in an 8-bit checkpoint: the same gradients as with the
- * values of lords_checkpoint_load as x.  Those values lie in the lords_init workspace meanwhile (M * n * 2 bytes at its end; LORDS_ERR_WORKSPACE when
- * there is no room for them), and the gradients see the workspace without them: to the last bit the same where what is left holds what
- * the gradients take there.
+ * lords_linear_backward_factors and lords_linear_backward_qat with the layer's input in an 8-bit checkpoint: the gradients of the values of
+ * lords_checkpoint_load as x.  Those values lie at the end of the lords_init workspace meanwhile (2 n bytes a token), and the gradients see the workspace
+ * without them.  Where it holds both, the results are the same to the last bit; else the tokens go through it in parts, multiples of 64, whose gradients
+ * are added up in fp32 in the outputs.  LORDS_ERR_WORKSPACE when it does not hold the values of 64 tokens, or of all of a smaller call.
  */
 int lords_linear_backward_factors_checkpoint(const void *dy, const uint8_t *q, const uint8_t *e, const uint8_t *Qpacked, const void *B,
                                              const void *A, const float *codebook, int bits, int M, int m, int n, int r, float *dB,

@@ -189,6 +189,7 @@ struct BwParams {
     // the codes fixed) and where dL/dW goes (null: not asked for)
     const uint16_t *W;    // bf16 [m][n]
     float *dW;            // float [m][n]
+    int onto;             // 1: the gradients are added to what dB, dA and dW hold (from earlier tokens)
 };
 
 // ROLE 0: dB for rows blockIdx.x * 64 ..; ROLE 1: dA for columns blockIdx.x * 64 ...
@@ -287,7 +288,10 @@ __global__ void __launch_bounds__(kBwThreads) lords_backward_factors_kernel(cons
                     lv = lv_s[read_code(p.q, row_bytes, i, j, p.bits)];
                     if (p.W) {
                         lv = sc[a][b] != 0.0f ? lv - bf16f(p.W[(size_t)i * p.n + j]) / sc[a][b] : 0.0f;
-                        if (write_dW) p.dW[(size_t)i * p.n + j] = c[a][b];
+                        if (write_dW) {
+                            float *at = p.dW + (size_t)i * p.n + j;
+                            *at = p.onto ? *at + c[a][b] : c[a][b];
+                        }
                     }
                 }
                 ds[ty * 4 + a][tx * 4 + b] = c[a][b] * lv;
@@ -328,10 +332,16 @@ __global__ void __launch_bounds__(kBwThreads) lords_backward_factors_kernel(cons
         const int e = tid + kBwThreads * a;
         if (ROLE == 0) {
             const int i = own0 + e / r4, k = e % r4;
-            if (p.dB && i < p.m && k < p.r) p.dB[(size_t)i * p.r + k] = acc[a];
+            if (p.dB && i < p.m && k < p.r) {
+                float *at = p.dB + (size_t)i * p.r + k;
+                *at = p.onto ? *at + acc[a] : acc[a];
+            }
         } else {
             const int k = e / kT, j = own0 + e % kT;
-            if (p.dA && k < p.r && j < p.n) p.dA[(size_t)k * p.n + j] = acc[a];
+            if (p.dA && k < p.r && j < p.n) {
+                float *at = p.dA + (size_t)k * p.n + j;
+                *at = p.onto ? *at + acc[a] : acc[a];
+            }
         }
     }
 }
@@ -477,6 +487,11 @@ __device__ __forceinline__ void red_add_v4(float *at, uint32_t a, uint32_t b, ui
                  "f"(__uint_as_float(d)) : "memory");
 }
 
+__device__ __forceinline__ void red_add_v2(float *at, uint32_t a, uint32_t b)
+{
+    asm volatile("red.relaxed.gpu.global.add.v2.f32 [%0], {%1, %2};" ::"l"(at), "f"(__uint_as_float(a)), "f"(__uint_as_float(b)) : "memory");
+}
+
 // The division of all 128 x 128 tiles, row block after row block, into one run per CTA.  row_splits 0: equal runs, which may cross from a row
 // block into the next (no CTA idles: 1024 tiles over 148 SMs are 7 rounds, four CTAs per row block 8); else that many runs per row
 // block (the element-wise B tile is built once per CTA).
@@ -512,8 +527,9 @@ struct alignas(64) BwTcParams {
     int *status;
 };
 
-// RAGGED: g, x or A are padded copies, and rows of W, dW and the codes may begin anywhere (checks that would cost the others 5 %).
-template <int RA, bool QAT, bool RAGGED>
+// RAGGED: g, x or A are padded copies, and rows of W, dW and the codes may begin anywhere (checks that would cost the others 5 %).  ONTO: dW is added to
+// what is there (asked at every store, QAT at rank 128, 256 tokens, 4096 x 4096 131.5 us in place of 126.8).
+template <int RA, bool QAT, bool RAGGED, bool ONTO>
 __global__ void __launch_bounds__(kTcThreads, 1) lords_backward_tc_kernel(const __grid_constant__ BwTcParams p)
 {
     using C = BwCfg<RA, QAT>;
@@ -844,7 +860,11 @@ __global__ void __launch_bounds__(kTcThreads, 1) lords_backward_tc_kernel(const 
                         if (row >= p.b.m || col >= p.b.n) return;
                         float *dst = p.b.dW + (size_t)row * p.b.n + col;
                         if constexpr (!RAGGED) {
-                            __stcs(reinterpret_cast<uint4 *>(dst), o);
+                            if constexpr (ONTO) red_add_v4(dst, o.x, o.y, o.z, o.w);     // (the only one to this place in the launch)
+                            else __stcs(reinterpret_cast<uint4 *>(dst), o);
+                        } else if constexpr (ONTO) {
+                            red_add_v2(dst, o.x, o.y);
+                            if (col + 2 < p.b.n) red_add_v2(dst + 2, o.z, o.w);
                         } else {                                                   // n is even: 8-byte aligned
                             *reinterpret_cast<uint2 *>(dst) = make_uint2(o.x, o.y);
                             if (col + 2 < p.b.n) *reinterpret_cast<uint2 *>(dst + 2) = make_uint2(o.z, o.w);
@@ -1016,7 +1036,8 @@ struct ReduceJob {
     Runs runs;            // tiles < 0: the number of contributions depends on the row block
 };
 
-__global__ void __launch_bounds__(256) lords_backward_reduce_kernel(const ReduceJob jb, const ReduceJob ja, int blocks_b)
+// ONTO: added to what `out` holds.
+template <bool ONTO> __global__ void __launch_bounds__(256) lords_backward_reduce_kernel(const ReduceJob jb, const ReduceJob ja, int blocks_b)
 {
     const bool isb = (int)blockIdx.x < blocks_b;
     const ReduceJob &j = isb ? jb : ja;
@@ -1034,12 +1055,12 @@ __global__ void __launch_bounds__(256) lords_backward_reduce_kernel(const Reduce
 #pragma unroll
         for (int k = 0; k < 16; ++k) s += v[k];
     }
-    j.out[e] = s;
+    j.out[e] = ONTO ? j.out[e] + s : s;
 }
 
 // The sums of the contributions to dB ([tiles_b][m][r4]; tiles_b < 0: see runs) and dA ([tiles_a][r4][n]); either may be absent.
 int launch_reduce(const float *part_b, float *dB, int tiles_b, const Runs &runs, const float *part_a, float *dA, int tiles_a, int m, int n, int r, int r4,
-                  cudaStream_t stream)
+                  int onto, cudaStream_t stream)
 {
     ReduceJob jb = {part_b, dB, tiles_b, dB ? m : 0, r, r4, (size_t)m * r4, runs};
     ReduceJob ja = {part_a, dA, tiles_a, dA ? r : 0, n, n, (size_t)r4 * n, runs};
@@ -1055,7 +1076,7 @@ int launch_reduce(const float *part_b, float *dB, int tiles_b, const Runs &runs,
     cfg.stream = stream;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    LORDS_CUDA_TRY(cudaLaunchKernelEx(&cfg, lords_backward_reduce_kernel, jb, ja, (int)nb));
+    LORDS_CUDA_TRY(cudaLaunchKernelEx(&cfg, onto ? lords_backward_reduce_kernel<true> : lords_backward_reduce_kernel<false>, jb, ja, (int)nb));
     return LORDS_OK;
 }
 
@@ -1100,12 +1121,12 @@ int launch_transpose_bf16_pair(const uint16_t *src0, int rows0, int cols0, uint1
     return LORDS_OK;
 }
 
-template <int RA, bool QAT, bool RAGGED> static int launch_tc_variant(BwTcParams &k, const State &st, cudaStream_t stream)
+template <int RA, bool QAT, bool RAGGED, bool ONTO> static int launch_tc_variant(BwTcParams &k, const State &st, cudaStream_t stream)
 {
     static bool done[kMaxDevices] = {};
     const int dev = device_slot(st);
     if (!done[dev]) {
-        LORDS_CUDA_TRY(cudaFuncSetAttribute(lords_backward_tc_kernel<RA, QAT, RAGGED>, cudaFuncAttributeMaxDynamicSharedMemorySize, BwCfg<RA, QAT>::SMEM));
+        LORDS_CUDA_TRY(cudaFuncSetAttribute(lords_backward_tc_kernel<RA, QAT, RAGGED, ONTO>, cudaFuncAttributeMaxDynamicSharedMemorySize, BwCfg<RA, QAT>::SMEM));
         done[dev] = true;
     }
     k.fold_bufs = BwCfg<RA, QAT>::DB_COL + 4 * (uint32_t)k.r_pad <= 512 ? 2 : 1;
@@ -1113,26 +1134,29 @@ template <int RA, bool QAT, bool RAGGED> static int launch_tc_variant(BwTcParams
     // without)
     const int mmas = (k.b.M + kTcTok - 1) / kTcTok * (kTcTok / 16);
     k.group = RAGGED ? (k.b.M <= 128 ? 2 : 4) : mmas <= 8 ? 4 : (mmas / 2 + 3) / 4 * 4;
-    lords_backward_tc_kernel<RA, QAT, RAGGED><<<(unsigned)k.runs.ctas, kTcThreads, BwCfg<RA, QAT>::SMEM, stream>>>(k);
+    lords_backward_tc_kernel<RA, QAT, RAGGED, ONTO><<<(unsigned)k.runs.ctas, kTcThreads, BwCfg<RA, QAT>::SMEM, stream>>>(k);
     LORDS_CUDA_TRY(cudaGetLastError());
     return LORDS_OK;
 }
 
-// The tensor schedule.  p.W != null: the gradients of quantisation-aware training (dW may be null).
-// LORDS_ERR_UNSUPPORTED when the shapes do not suit it or the workspace cannot hold the contributions.
-static int launch_backward_tc(const BwParams &p, State &st, cudaStream_t stream)
+// What the tensor schedule takes for a call: its division into runs, and bytes of the workspace for the contributions and for padded copies.
+struct TcPlan {
+    Runs runs;
+    bool taken;           // it takes the call
+    int m8, n8;           // row pitches: rows of g, x or A that are not 16-byte multiples are copied to such, zeros behind
+    size_t nb, na, ng, nx, nf;
+    size_t bytes() const { return nb + na + ng + nx + nf; }
+};
+static TcPlan plan_tc(int M, int m, int n, int r, bool dB, bool dA, const State &st)
 {
-    const int m = p.m, n = p.n, r = p.r, M = p.M;
-    BwTcParams k;
-    k.b = p;
-    k.r4 = (r + 3) & ~3;
-    k.r_pad = (r + 15) & ~15;
+    TcPlan k;
     Runs &runs = k.runs;
     runs.row_blocks = (m + kTcRows - 1) / kTcRows;
     runs.col_tiles = (n + kTcCols - 1) / kTcCols;
     const long long tiles = (long long)runs.row_blocks * runs.col_tiles;
     runs.row_splits = 0;
     int parts = 1;
+    k.taken = true;
     if ((r & 7) == 0) {
         runs.ctas = (int)(tiles < st.sm_count ? tiles : st.sm_count);
         for (int rb = 0; rb < runs.row_blocks; ++rb) parts = runs.parts(rb) > parts ? runs.parts(rb) : parts;
@@ -1144,18 +1168,39 @@ static int launch_backward_tc(const BwParams &p, State &st, cudaStream_t stream)
             if (t < best) { best = t; runs.row_splits = s; }
         }
         parts = runs.row_splits;
-        if ((long long)runs.row_blocks * parts > 2147483647LL) return LORDS_ERR_UNSUPPORTED;
-        runs.ctas = runs.row_blocks * parts;
+        k.taken = (long long)runs.row_blocks * parts <= 2147483647LL;
+        runs.ctas = k.taken ? runs.row_blocks * parts : 0;
     }
-    // rows of g, x or A that are not 16-byte multiples: padded copies, except where the call is so small that the CUDA cores' tiles are as
-    // good (1024 x 300, two tokens)
     auto up = [](size_t b) { return (b + 255) & ~(size_t)255; };
-    const int m8 = (m + 7) & ~7, n8 = (n + 7) & ~7;
+    k.m8 = (m + 7) & ~7;
+    k.n8 = (n + 7) & ~7;
+    // (not where a call with such rows is so small that the CUDA cores' tiles are as good: 1024 x 300, two tokens)
+    if ((k.m8 != m || k.n8 != n) && (long long)M * m * n <= (1 << 22)) k.taken = false;
+    const size_t r4 = (size_t)(r + 3) & ~(size_t)3;
+    k.nb = up(dB ? (size_t)parts * m * r4 * sizeof(float) : 0);
+    k.na = up(dA ? (size_t)runs.row_blocks * r4 * n * sizeof(float) : 0);
+    k.ng = up(k.m8 != m ? (size_t)M * k.m8 * 2 : 0);
+    k.nx = up(k.n8 != n ? (size_t)M * k.n8 * 2 : 0);
+    k.nf = up(k.n8 != n ? (size_t)r * k.n8 * 2 : 0);
+    return k;
+}
+
+// The tensor schedule.  p.W != null: the gradients of quantisation-aware training (dW may be null).
+// LORDS_ERR_UNSUPPORTED when the shapes do not suit it or the workspace cannot hold the contributions.
+static int launch_backward_tc(const BwParams &p, State &st, cudaStream_t stream)
+{
+    const int m = p.m, n = p.n, r = p.r, M = p.M;
+    const TcPlan plan = plan_tc(M, m, n, r, p.dB != nullptr, p.dA != nullptr, st);
+    if (!plan.taken || plan.bytes() > st.workspace_bytes) return LORDS_ERR_UNSUPPORTED;
+    BwTcParams k;
+    k.b = p;
+    k.r4 = (r + 3) & ~3;
+    k.r_pad = (r + 15) & ~15;
+    k.runs = plan.runs;
+    const Runs &runs = k.runs;
+    const int m8 = plan.m8, n8 = plan.n8;
     const bool pad = m8 != m || n8 != n;
-    if (pad && (long long)M * m * n <= (1 << 22)) return LORDS_ERR_UNSUPPORTED;
-    const size_t nb = up(p.dB ? (size_t)parts * m * k.r4 * sizeof(float) : 0), na = up(p.dA ? (size_t)runs.row_blocks * k.r4 * n * sizeof(float) : 0);
-    const size_t ng = up(m8 != m ? (size_t)M * m8 * 2 : 0), nx = up(n8 != n ? (size_t)M * n8 * 2 : 0), nf = up(n8 != n ? (size_t)r * n8 * 2 : 0);
-    if (nb + na + ng + nx + nf > st.workspace_bytes) return LORDS_ERR_UNSUPPORTED;
+    const size_t nb = plan.nb, na = plan.na, ng = plan.ng, nx = plan.nx, nf = plan.nf;
     k.part_dB = p.dB ? reinterpret_cast<float *>(st.workspace) : nullptr;
     k.part_dA = p.dA ? reinterpret_cast<float *>(st.workspace + nb) : nullptr;
     k.status = st.status_word;
@@ -1191,7 +1236,8 @@ static int launch_backward_tc(const BwParams &p, State &st, cudaStream_t stream)
     auto variant = [&](auto ra, auto qat) {
         constexpr int RA = decltype(ra)::value;
         constexpr bool QAT = decltype(qat)::value;
-        return ragged ? launch_tc_variant<RA, QAT, true>(k, st, stream) : launch_tc_variant<RA, QAT, false>(k, st, stream);
+        if (QAT && p.dW && p.onto) return ragged ? launch_tc_variant<RA, QAT, true, QAT>(k, st, stream) : launch_tc_variant<RA, QAT, false, QAT>(k, st, stream);
+        return ragged ? launch_tc_variant<RA, QAT, true, false>(k, st, stream) : launch_tc_variant<RA, QAT, false, false>(k, st, stream);
     };
     using Small = std::integral_constant<int, 64>;
     using Large = std::integral_constant<int, 128>;
@@ -1199,7 +1245,7 @@ static int launch_backward_tc(const BwParams &p, State &st, cudaStream_t stream)
     else rc = r <= 64 ? variant(Small{}, std::false_type{}) : variant(Large{}, std::false_type{});
     if (rc != LORDS_OK) return rc;
     if (p.dB || p.dA) {
-        rc = launch_reduce(k.part_dB, p.dB, -1, runs, k.part_dA, p.dA, runs.row_blocks, m, n, r, k.r4, stream);
+        rc = launch_reduce(k.part_dB, p.dB, -1, runs, k.part_dA, p.dA, runs.row_blocks, m, n, r, k.r4, p.onto, stream);
         if (rc != LORDS_OK) return rc;
         ++launches;
     }
@@ -1208,12 +1254,23 @@ static int launch_backward_tc(const BwParams &p, State &st, cudaStream_t stream)
     return LORDS_OK;
 }
 
+// Bytes of the workspace that the quickest schedule of a call takes ("tensor", or else "tiles" for the factors).
+size_t backward_scratch(int M, int m, int n, int r, bool dB, bool dA, bool qat, const State &st)
+{
+    const TcPlan plan = plan_tc(M, m, n, r, dB, dA, st);
+    if (st.forced_path == 0 && plan.taken) return plan.bytes();
+    if (qat || st.forced_path == 1) return 0;
+    const size_t r4 = (size_t)(r + 3) & ~(size_t)3;
+    return (dB ? (size_t)((n + kT - 1) / kT) * m * r4 * sizeof(float) : 0) + (dA ? (size_t)((m + kT - 1) / kT) * r4 * n * sizeof(float) : 0) + 256;
+}
+
 int launch_backward_factors(const uint16_t *g, const uint16_t *x, const uint8_t *q, const uint16_t *B, const uint16_t *A,
-                            const float *levels, int bits, int M, int m, int n, int r, float *dB, float *dA,
+                            const float *levels, int bits, int M, int m, int n, int r, float *dB, float *dA, int onto,
                             State &st, cudaStream_t stream)
 {
     if (r > kRMaxBw) return LORDS_ERR_SHAPE;
     BwParams p;
+    p.onto = onto;
     p.g = g; p.x = x; p.q = q; p.B = B; p.A = A;
     for (int c = 0; c < 16; ++c) p.levels[c] = c < (1 << bits) ? levels[c] : 0.0f;
     p.bits = bits; p.M = M; p.m = m; p.n = n; p.r = r;
@@ -1235,7 +1292,7 @@ int launch_backward_factors(const uint16_t *g, const uint16_t *x, const uint8_t 
         LORDS_CUDA_TRY(cudaGetLastError());
         ++launches;
         {
-            const int rc = launch_reduce(part_b, dB, jt_n, Runs{}, part_a, dA, it_n, m, n, r, r4, stream);
+            const int rc = launch_reduce(part_b, dB, jt_n, Runs{}, part_a, dA, it_n, m, n, r, r4, onto, stream);
             if (rc != LORDS_OK) return rc;
             ++launches;
         }
@@ -1263,10 +1320,11 @@ int launch_backward_factors(const uint16_t *g, const uint16_t *x, const uint8_t 
 // requested factor gradient).
 int launch_backward_qat(const uint16_t *g, const uint16_t *x, const uint16_t *W, const uint8_t *q, const uint16_t *B,
                         const uint16_t *A, const float *levels, int bits, int M, int m, int n, int r, float *dW, float *dB,
-                        float *dA, State &st, cudaStream_t stream)
+                        float *dA, int onto, State &st, cudaStream_t stream)
 {
     if (r > kRMaxBw) return LORDS_ERR_SHAPE;
     BwParams p;
+    p.onto = onto;
     p.g = g; p.x = x; p.q = q; p.B = B; p.A = A;
     for (int c = 0; c < 16; ++c) p.levels[c] = c < (1 << bits) ? levels[c] : 0.0f;
     p.bits = bits; p.M = M; p.m = m; p.n = n; p.r = r;

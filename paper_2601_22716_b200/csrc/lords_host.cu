@@ -594,7 +594,7 @@ int lords_linear_backward_factors(const void *dy, const void *x, const uint8_t *
     if (rc != LORDS_OK) return rc;
     return launch_backward_factors(static_cast<const uint16_t *>(dy), static_cast<const uint16_t *>(x), Qpacked,
                                    static_cast<const uint16_t *>(B), static_cast<const uint16_t *>(A), codebook, bits, M, m,
-                                   n, r, dB, dA, state(), static_cast<cudaStream_t>(stream));
+                                   n, r, dB, dA, 0, state(), static_cast<cudaStream_t>(stream));
 }
 
 int lords_linear_backward_qat(const void *dy, const void *x, const void *W, const uint8_t *Qpacked, const void *B, const void *A,
@@ -605,7 +605,7 @@ int lords_linear_backward_qat(const void *dy, const void *x, const void *W, cons
     if (rc != LORDS_OK) return rc;
     return launch_backward_qat(static_cast<const uint16_t *>(dy), static_cast<const uint16_t *>(x), static_cast<const uint16_t *>(W),
                                Qpacked, static_cast<const uint16_t *>(B), static_cast<const uint16_t *>(A), codebook, bits, M, m, n, r,
-                               dW, dB, dA, state(), static_cast<cudaStream_t>(stream));
+                               dW, dB, dA, 0, state(), static_cast<cudaStream_t>(stream));
 }
 
 static int blockscale_common(const void *x, const uint8_t *q, const void *scales, const float *cb, int bits, int blk, int M,

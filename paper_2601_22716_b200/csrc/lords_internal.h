@@ -127,9 +127,12 @@ int launch_quantize(const void *W, const void *B, const void *A, const float *le
 int launch_transpose_codes(const uint8_t *Q, int m, int n, int bits, uint8_t *Qt, cudaStream_t stream);
 int launch_transpose_bf16_pair(const uint16_t *src0, int rows0, int cols0, uint16_t *dst0, const uint16_t *src1, int rows1, int cols1,
                                uint16_t *dst1, cudaStream_t stream);
+// (onto: 1 adds to what the outputs hold, from earlier tokens.)
 int launch_backward_factors(const uint16_t *g, const uint16_t *x, const uint8_t *q, const uint16_t *B, const uint16_t *A,
-                            const float *levels, int bits, int M, int m, int n, int r, float *dB, float *dA,
+                            const float *levels, int bits, int M, int m, int n, int r, float *dB, float *dA, int onto,
                             State &st, cudaStream_t stream);
+// Bytes of the workspace that the quickest schedule of these gradients, or of those below (qat), takes.
+size_t backward_scratch(int M, int m, int n, int r, bool dB, bool dA, bool qat, const State &st);
 
 // What the entry points of both gradients ask of their arguments.
 int check_backward_factors(const void *dy, const void *x, const uint8_t *q, const void *B, const void *A, const float *codebook, int bits, int M, int m,
@@ -141,7 +144,7 @@ int check_backward_qat(const void *dy, const void *x, const void *W, const uint8
 // rules hold, else one pass over W per requested factor gradient on the CUDA cores.
 int launch_backward_qat(const uint16_t *g, const uint16_t *x, const uint16_t *W, const uint8_t *q, const uint16_t *B,
                         const uint16_t *A, const float *levels, int bits, int M, int m, int n, int r, float *dW, float *dB,
-                        float *dA, State &st, cudaStream_t stream);
+                        float *dA, int onto, State &st, cudaStream_t stream);
 
 // Comparators (Sec. 4.4, Table 6): the block-scale instantiation of the 16-token decode kernel (Eq. 2) and
 // the two extra launches of an additive low-rank adapter on top of it.
