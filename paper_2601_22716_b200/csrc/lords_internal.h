@@ -178,7 +178,8 @@ template <class Kernel, class... Args> inline int launch_dependent(Kernel kernel
 }
 int launch_mxfp4_quantize(const uint16_t *v, int rows, int cols, uint8_t *codes, uint8_t *scales, uint8_t *codes_t, uint8_t *scales_t, cudaStream_t stream);
 int launch_mxfp4_dequantize(const uint8_t *codes, const uint8_t *scales, int rows, int cols, uint16_t *v, cudaStream_t stream);
-// Few tokens: a CTA per 128 rows of W, the steps divided among a cluster.  x in bf16 (up to four tokens; else LORDS_ERR_UNSUPPORTED) or in 4 bits.
+// Few tokens: a CTA per 128 rows of W, the steps divided among a cluster.  x in 4 bits, or in bf16: up to four tokens, and up to 64 where tokens x steps of
+// a CTA are at most 64 (else LORDS_ERR_UNSUPPORTED).
 int launch_mxfp4_stream(const MxProblem &p, State &st, cudaStream_t stream);
 // Many tokens: CTA pairs, 256 tokens x 128 or 256 out-features.  x in 4 bits.
 int launch_mxfp4_pair(const MxProblem &p, State &st, cudaStream_t stream);

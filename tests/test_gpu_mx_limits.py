@@ -92,6 +92,22 @@ def test_a_call_of_one_launch_needs_no_workspace(M, n):
         lords.lords_init(0, 0)
 
 
+# One row tile.  256 columns are one step: one launch up to 64 tokens.  12000 columns are 47 steps, six a CTA of eight: one launch up to four tokens, and
+# up to ten (64 tokens x steps a CTA).
+@pytest.mark.parametrize("m,n,M,launches", [(100, 256, 1, 1), (100, 256, 5, 1), (100, 256, 16, 1), (100, 256, 32, 1), (100, 256, 64, 1), (100, 256, 65, 2), (70, 12000, 1, 1),
+                                            (70, 12000, 4, 1), (70, 12000, 10, 1), (70, 12000, 11, 2), (70, 12000, 16, 2), (70, 12000, 33, 2), (70, 12000, 64, 2)])
+def test_launches_of_a_layer(m, n, M, launches):
+    x, w = _normal(M, n, 1), _normal(m, n, 2)
+    xq, wq = _four(M, n), _four(m, n)
+    lords.lords_mxfp4_quantize(x, M, n, *xq)
+    lords.lords_mxfp4_quantize(w, m, n, *wq)
+    a, b = torch.empty(M, m, device="cuda"), torch.empty(M, m, device="cuda")
+    lords.lords_mxfp4_matmul(*xq, *wq, M, m, n, a, f32=True)
+    lords.lords_mxfp4_forward(x, *wq, M, m, n, b, f32=True)
+    assert lords.lords_last_launch_count() == launches
+    assert torch.equal(a, b)
+
+
 FIRST = """
 import threading
 import torch
