@@ -123,7 +123,7 @@ __device__ __forceinline__ bool sums_read(bool in_vain)
 }
 
 // The sums of a row (y: where its value of token 0 goes, `inside`: it is a row of W) as the one CTA of a tile has them.
-template <int BN, class T> __device__ __forceinline__ void write_out(uint32_t acc, int tokens, T *y, int m, bool inside)
+template <class T> __device__ __forceinline__ void write_out(uint32_t acc, int tokens, T *y, int m, bool inside)
 {
     const size_t pitch = (size_t)m;
 #pragma unroll 1
@@ -142,7 +142,7 @@ template <int BN, class T> __device__ __forceinline__ void write_out(uint32_t ac
 // The cluster's sums: tokens in groups of GW, group g to rank g mod cluster; a received value's place is (group / cluster, rank, row).
 // (64 tokens of 1024 x 1024 on two CTAs 4.1 us, 3.3 on one.  Level or slower: the tokens on eight warps, all ranks' values loaded at once; by copies in bulk from
 // shared memory, with a wait for them at the end, 4.45.)
-template <int BN, int GW, class T>
+template <int GW, class T>
 __device__ __forceinline__ bool add_up(uint32_t acc, uint32_t recv, uint32_t bar_recv, int rank, int split, int tokens, T *y, int m, bool inside, int ri,
                                        const int *status, bool failed)
 {
@@ -380,13 +380,13 @@ __global__ void __launch_bounds__(SCfg<BN, QX>::THREADS, 1) lords_mxfp4_stream_k
             auto out = [&](auto *base) {
                 auto *y = base + (size_t)tok0 * p.m + i;
                 if (split <= 1) {
-                    if (!failed) write_out<BN>(acc, tokens, y, p.m, i < p.m);
+                    if (!failed) write_out(acc, tokens, y, p.m, i < p.m);
                     sums_read(failed);
                     return;
                 }
-                const bool ok = gw == 4   ? add_up<BN, 4>(acc, recv, bar_recv, rank, split, tokens, y, p.m, i < p.m, ri, status, failed)
-                                : gw == 2 ? add_up<BN, 2>(acc, recv, bar_recv, rank, split, tokens, y, p.m, i < p.m, ri, status, failed)
-                                          : add_up<BN, 1>(acc, recv, bar_recv, rank, split, tokens, y, p.m, i < p.m, ri, status, failed);
+                const bool ok = gw == 4   ? add_up<4>(acc, recv, bar_recv, rank, split, tokens, y, p.m, i < p.m, ri, status, failed)
+                                : gw == 2 ? add_up<2>(acc, recv, bar_recv, rank, split, tokens, y, p.m, i < p.m, ri, status, failed)
+                                          : add_up<1>(acc, recv, bar_recv, rank, split, tokens, y, p.m, i < p.m, ri, status, failed);
                 alone = !ok;
                 failed = failed || alone;
             };
