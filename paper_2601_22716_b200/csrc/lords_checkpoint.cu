@@ -1,7 +1,8 @@
 // Activations kept for the backward pass in 8 bits (the format of lords_mx.cuh: whole numbers -127 .. 127 in steps of 1/64, a scale 2^E per 32
 // values of a token), and taken up again in bf16.  A value of the format is a bf16 number, so only the store rounds.
 //
-// A block is four neighbouring threads of eight values each.  Bound: the bytes, 2 + 33/32 a value either way.
+// A thread has sixteen values, half a block, or eight on the way out into rows that do not begin at 32-byte boundaries.  Bound: the bytes, 2 + 33/32 a value
+// either way.
 #include <cuda_bf16.h>
 
 #include "lords_internal.h"
